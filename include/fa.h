@@ -205,6 +205,84 @@ int fa_aggregate_host(const void* G_host, int dtype, int p, long long n, int m, 
 #define FA_STATIC_MAX_BLOCKS 160
 int fa_gram_static(const void* G, int dtype, int p, long long n, double* K, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Training operators: what a worker needs next to the aggregation to produce its row of G.  Layer
+ * norm with its gradient, activation checkpoints in 8 bits, and the backward passes that read such
+ * checkpoints.  Parameter gradients are written as plain contiguous vectors or matrices of type
+ * fp32 or bf16 with no alignment beyond their element's, so they can be parts of a row of G.
+ *
+ * Activations are rows x cols matrices with unit column stride and a row stride (ld*, in elements);
+ * a row stride of 0 is allowed for inputs (one row for all).  dtype is the type of every activation
+ * of a call, pdtype that of its parameter vectors, gdtype that of its parameter gradients.  Sums,
+ * means and all arithmetic are fp32; every output is rounded once, to nearest even.  0 <= rows <=
+ * FA_MAX_ROWS, 1 <= cols <= FA_MAX_COLS; with rows = 0 gradients of parameters are written as zeros.
+ * The ownership, ordering and error rules above hold; outputs may not overlap inputs or each other.
+ * Non-finite values run through as the formulas say.
+ *
+ * Checkpoint: every row is cut into groups of 32 values (the last one filled up with zeros).  A group
+ * has the scale 2^e, e the smallest integer >= -127 with 127 * 2^e >= its largest magnitude; a value v
+ * is held as the int8 code rint(v / 2^e), half to even, and reads back as code * 2^e: off by at most
+ * 2^(e-1), which is at most 1/126 of the group's largest magnitude (for magnitudes from 127 * 2^-127
+ * on).  At e = 122, the largest, codes end at +-63, so that finite values stay finite.  A group with
+ * an Inf or NaN reads back as NaN.  Buffer, 16-byte aligned, fa_checkpoint8_bytes()
+ * long: codes [rows][32 * groups], then from the next multiple of 256 bytes the scales as bytes e + 127
+ * (255: Inf or NaN in the group), [rows][groups rounded up to a multiple of 4]. */
+#define FA_MAX_ROWS (1LL << 40)
+#define FA_MAX_COLS (1LL << 23)
+
+int fa_checkpoint8_bytes(long long rows, long long cols, size_t* bytes);
+int fa_checkpoint8_store(const void* x, long long ldx, int dtype, long long rows, long long cols, void* ck,
+                         void* stream);
+int fa_checkpoint8_load(const void* ck, int dtype, long long rows, long long cols, void* out, long long ldo,
+                        void* stream);
+
+/* Layer norm over the columns.  s = x + residual (residual may be NULL: s = x),
+ *   mean = sum(s) / cols, rstd = 1 / sqrt(sum((s - mean)^2) / cols + eps), y = (s - mean) * rstd * weight + bias.
+ *   weight, bias : cols values or NULL (1 and 0);  eps >= 0, finite
+ *   sum_out      : s, or NULL;  mean, rstd : rows floats each, or NULL
+ *   ck_sum, ck_y : checkpoints of s and of y as they are stored in type dtype, or NULL */
+int fa_layer_norm_forward(const void* x, long long ldx, const void* residual, long long ldr, int dtype,
+                          long long rows, long long cols, const void* weight, const void* bias, int pdtype,
+                          float eps, void* y, long long ldy, void* sum_out, long long lds, float* mean,
+                          float* rstd, void* ck_sum, void* ck_y, void* stream);
+
+/* Its gradient.  h = (s - mean) * rstd, g = dy * weight:
+ *   dx = rstd * (g - mean(g) - h * mean(g * h)) + residual_grad  (the gradient of x and of residual alike),
+ *   dweight = sum over rows of dy * h, dbias = sum over rows of dy.
+ * s is given as x (type dtype) or as a checkpoint ck, the other one NULL.  residual_grad, dweight and
+ * dbias may be NULL.  ws: fa_layer_norm_backward_workspace_bytes(). */
+int fa_layer_norm_backward_workspace_bytes(long long rows, long long cols, size_t* bytes);
+int fa_layer_norm_backward(const void* dy, long long lddy, const void* x, long long ldx, const void* ck, int dtype,
+                           long long rows, long long cols, const void* weight, int pdtype, const float* mean,
+                           const float* rstd, const void* residual_grad, long long ldr, void* dx, long long lddx,
+                           void* dweight, void* dbias, int gdtype, void* ws, size_t ws_bytes, void* stream);
+
+/* y = gelu(z), z = x + bias (bias may be NULL).
+ *   approximate : FA_GELU_ERF z * Phi(z), Phi the normal distribution function;
+ *                 FA_GELU_TANH z * (1 + tanh(sqrt(2/pi) * (z + 0.044715 z^3))) / 2
+ *   ck_x, ck_y  : checkpoints of z (before any rounding) and of y as it is stored, or NULL */
+#define FA_GELU_ERF  0
+#define FA_GELU_TANH 1
+int fa_gelu_forward(const void* x, long long ldx, int dtype, long long rows, long long cols, const void* bias,
+                    int pdtype, int approximate, void* y, long long ldy, void* ck_x, void* ck_y, void* stream);
+
+/* dx = dy * gelu'(z), dbias = sum over rows of dx (before its rounding; NULL: not wanted).  z is x + bias,
+ * or what the checkpoint ck holds (x and bias NULL then).  ws (only read with dbias):
+ * fa_gelu_backward_workspace_bytes(). */
+int fa_gelu_backward_workspace_bytes(long long rows, long long cols, size_t* bytes);
+int fa_gelu_backward(const void* dy, long long lddy, const void* x, long long ldx, const void* bias, int pdtype,
+                     const void* ck, int dtype, long long rows, long long cols, int approximate, void* dx,
+                     long long lddx, void* dbias, int gdtype, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradient of a linear layer's weight and bias from the checkpoint of its input X (rows x ins):
+ *   dweight[o][i] = sum over rows t of dy[t][o] * X[t][i]   (outs x ins, contiguous),
+ *   dbias[o] = sum over rows t of dy[t][o]                  (NULL: not wanted).
+ * Products are exact, sums fp32.  ws: fa_linear_weight_grad_workspace_bytes(). */
+int fa_linear_weight_grad_workspace_bytes(long long rows, long long outs, long long ins, int dtype, size_t* bytes);
+int fa_linear_weight_grad(const void* dy, long long lddy, int dtype, long long rows, long long outs, const void* ck,
+                          long long ins, void* dweight, void* dbias, int gdtype, void* ws, size_t ws_bytes,
+                          void* stream);
+
 /* Static text for a host return code. */
 const char* fa_error_string(int code);
 

@@ -376,3 +376,10 @@ def fa_aggregate_host(G_host, m, lam, iters, out_host, G_dev, out_dev, ws, statu
         _check(_lib.fa_aggregate_host(args_host[0], code, p, n, m, float(lam), iters, args_host[1], args_host[2],
                                       Gd, od, wp, wb, sd, st), "fa_aggregate_host")
     return out_host
+
+
+from .training import (  # noqa: E402  (needs the helpers above)
+    fa_checkpoint8_bytes, fa_checkpoint8_load, fa_checkpoint8_store, fa_gelu_backward,
+    fa_gelu_backward_workspace_bytes, fa_gelu_forward, fa_layer_norm_backward,
+    fa_layer_norm_backward_workspace_bytes, fa_layer_norm_forward, fa_linear_weight_grad,
+    fa_linear_weight_grad_workspace_bytes, new_checkpoint8)

@@ -1,0 +1,218 @@
+// Activations in chunks of 8 elements, and the 8-bit checkpoint format.
+//
+// Format: a row is cut into groups of 32 values (the last one filled up with zeros).  A group has the
+// scale 2^e, e the smallest integer >= -127 with 127 * 2^e >= its largest magnitude, and every value is
+// held as the int8 code rint(v / 2^e) (half to even).  With a power of two as the scale
+//   * v / 2^e is exact, so the codes depend on the values alone and not on how they were computed, and
+//   * code * 2^e has at most 7 significant bits and is exact in bf16, so the tensor cores take it as an
+//     operand without a second rounding.
+// A linear scale (largest magnitude / 127) would use the codes' range fully (on average 0.7 of it is
+// used here) but has neither property.  The scale is kept as the byte e + 127; 255 marks a group that
+// holds an Inf or a NaN: it reads back as NaN everywhere, so that a broken activation stays visible.
+// At e = 122, the largest, codes end at +-63: what is finite stays finite.
+//
+// Buffer: codes [rows][32 * groups], then, from the next multiple of 256 bytes, scale bytes
+// [rows][groups rounded up to 4] (32-bit loads cover four groups of a row).
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace fa {
+
+using bf16 = __nv_bfloat16;
+
+__host__ __device__ inline long long act8_groups(long long cols) { return (cols + 31) / 32; }
+__host__ __device__ inline long long act8_scale_pitch(long long cols) { return (act8_groups(cols) + 3) / 4 * 4; }
+__host__ __device__ inline long long act8_scale_offset(long long rows, long long cols) {
+  return (rows * act8_groups(cols) * 32 + 255) / 256 * 256;
+}
+
+// Part of a checkpoint a kernel works on: `codes` and `scales` point at its first row.
+struct Act8 {
+  uint8_t* codes;
+  uint8_t* scales;
+};
+
+// ---- 8 elements <-> floats.  VEC: rows start on 16-byte boundaries and cols is a multiple of 8, so a
+// chunk is whole or absent; otherwise elements are moved one by one up to the row's end.
+__device__ __forceinline__ float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<uint32_t*>(&t);
+}
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(bf16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ bf16 from_float<bf16>(float v) { return __float2bfloat16_rn(v); }
+
+template <typename T> struct Raw8;
+template <> struct Raw8<bf16> {
+  uint4 u;
+  __device__ __forceinline__ void zero() { u = make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    v[0] = bf16_lo(u.x); v[1] = bf16_hi(u.x); v[2] = bf16_lo(u.y); v[3] = bf16_hi(u.y);
+    v[4] = bf16_lo(u.z); v[5] = bf16_hi(u.z); v[6] = bf16_lo(u.w); v[7] = bf16_hi(u.w);
+  }
+  __device__ __forceinline__ void put(const float (&v)[8]) {
+    u = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+  }
+  __device__ __forceinline__ void load(const bf16* p) { u = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void store(bf16* p) const { *reinterpret_cast<uint4*>(p) = u; }
+};
+template <> struct Raw8<float> {
+  float4 a, b;
+  __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+  __device__ __forceinline__ void put(const float (&v)[8]) {
+    a = make_float4(v[0], v[1], v[2], v[3]); b = make_float4(v[4], v[5], v[6], v[7]);
+  }
+  __device__ __forceinline__ void load(const float* p) {
+    a = *reinterpret_cast<const float4*>(p); b = *reinterpret_cast<const float4*>(p + 4);
+  }
+  __device__ __forceinline__ void store(float* p) const {
+    *reinterpret_cast<float4*>(p) = a; *reinterpret_cast<float4*>(p + 4) = b;
+  }
+};
+
+// Elements c*8 .. c*8+7 of a row, zeros past its end.
+template <typename T, bool VEC>
+__device__ __forceinline__ Raw8<T> load_chunk(const T* row, int c, int cols) {
+  Raw8<T> r;
+  const int j = c * 8;
+  if constexpr (VEC) {
+    if (j < cols) r.load(row + j);
+    else r.zero();
+  } else {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = j + i < cols ? to_float(row[j + i]) : 0.f;
+    r.put(v);      // exact: the values have T's precision
+  }
+  return r;
+}
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void store_chunk(T* row, int c, int cols, const float (&v)[8]) {
+  const int j = c * 8;
+  if constexpr (VEC) {
+    if (j < cols) {
+      Raw8<T> r;
+      r.put(v);
+      r.store(row + j);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (j + i < cols) row[j + i] = from_float<T>(v[i]);
+  }
+}
+
+// Parameter vectors (weight, bias): type known at run time, one element at a time or 16 bytes at once.
+struct ParamVec {
+  const void* p;       // null: the constant `none`
+  int is_bf16;
+  int vec;             // 16-byte aligned and a multiple of 8 long
+};
+__device__ __forceinline__ void load_param(const ParamVec& w, int c, int cols, float none, float (&v)[8]) {
+  const int j = c * 8;
+  if (!w.p || j >= cols) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = none;
+  } else if (w.vec) {
+    if (w.is_bf16) { Raw8<bf16> r; r.load(static_cast<const bf16*>(w.p) + j); r.get(v); }
+    else { Raw8<float> r; r.load(static_cast<const float*>(w.p) + j); r.get(v); }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[i] = none;
+      if (j + i < cols)
+        v[i] = w.is_bf16 ? to_float(static_cast<const bf16*>(w.p)[j + i]) : static_cast<const float*>(w.p)[j + i];
+    }
+  }
+}
+
+// Values as they stand in memory of type T.
+template <typename T>
+__device__ __forceinline__ void round_to(float (&v)[8]) {
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = to_float(from_float<T>(v[i]));
+  }
+}
+
+// ---- encode: the four lanes of an aligned quad hold one group, 8 values each.  All 32 lanes call.
+__device__ __forceinline__ uint32_t act8_scale_byte(uint32_t amax_bits) {
+  // 127 * 2^e = 1.984375 * 2^(e+6): adding 2^17 - 1 carries into the exponent when the mantissa is above that
+  const uint32_t k = (amax_bits + 0x1FFFFu) >> 23;
+  return amax_bits >= 0x7F800000u ? 255u : (k > 6u ? k - 6u : 0u);
+}
+__device__ __forceinline__ float act8_scale(uint32_t byte) {
+  return byte == 255u ? __uint_as_float(0x7FC00000u) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
+}
+
+__device__ __forceinline__ uint2 act8_encode(const float (&v)[8], uint32_t* byte_out) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);   // NaN and Inf compare above all else
+  m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+  m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+  const uint32_t byte = act8_scale_byte(m);
+  *byte_out = byte;
+  const float inv = __uint_as_float((254u - byte) << 23);        // 2^-e, exact (byte <= 249 or 255)
+  const float top = byte == 249u ? 63.f : 127.f;                 // 64 * 2^122 is past the largest float
+  uint32_t q[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)                                    // 1.5 * 2^23: rint in the low byte
+    q[i] = __float_as_uint(fminf(fmaxf(v[i] * inv, -top), top) + 12582912.f);
+  uint2 r;
+  r.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+  r.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
+  if (byte == 255u) r = make_uint2(0, 0);
+  return r;
+}
+
+// Codes and scale of chunk c of a row; the lane of the row's last group also clears the scales' padding.
+__device__ __forceinline__ void act8_put(uint8_t* codes_row, uint8_t* scales_row, int c, int groups, const float (&v)[8],
+                                         bool valid) {
+  uint32_t byte;
+  const uint2 q = act8_encode(v, &byte);
+  if (!valid) return;
+  *reinterpret_cast<uint2*>(codes_row + (size_t)c * 8) = q;
+  if ((c & 3) == 0) {
+    const int g = c >> 2;
+    scales_row[g] = static_cast<uint8_t>(byte);
+    if (g == groups - 1)
+      for (int i = groups; i & 3; ++i) scales_row[i] = 0;
+  }
+}
+
+// ---- decode
+__device__ __forceinline__ void act8_decode(uint2 q, uint32_t byte, float (&v)[8]) {
+  const float s = act8_scale(byte);
+  const uint32_t a = q.x ^ 0x80808080u, b = q.y ^ 0x80808080u;   // code + 128 as an unsigned byte
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {                                 // 2^23 + (code + 128) by its bits, minus the offset: exact
+    v[i] = (__uint_as_float(__byte_perm(a, 0x4B000000u, 0x7440 + i)) - 8388736.f) * s;
+    v[4 + i] = (__uint_as_float(__byte_perm(b, 0x4B000000u, 0x7440 + i)) - 8388736.f) * s;
+  }
+}
+
+// ---- division by a number fixed per launch, for 0 <= n < 2^31
+struct FastDiv {
+  uint32_t d, mul, shift;
+  explicit FastDiv(uint32_t div = 1) : d(div), mul(0), shift(0) {
+    while ((1ull << shift) < div) ++shift;
+    // m = floor(2^32 (2^shift - d) / d) + 1;  n / d = (umulhi(n, m) + n) >> shift
+    mul = static_cast<uint32_t>(((1ull << 32) * ((1ull << shift) - div)) / div + 1);
+  }
+  __device__ __forceinline__ uint32_t div(uint32_t n) const {
+    return static_cast<uint32_t>((static_cast<uint64_t>(__umulhi(n, mul)) + n) >> shift);
+  }
+};
+
+}  // namespace fa
