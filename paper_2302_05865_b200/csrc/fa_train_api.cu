@@ -30,6 +30,10 @@ bool out_ok(const void* p, long long ld, long long rows, long long cols) {
 
 int cuda_code(cudaError_t e) { return e == cudaSuccess ? FA_OK : FA_ERR_CUDA; }
 
+// A product: tokens are counted in 32 bits on the device, and the result has to fit some memory.
+bool product_ok(long long rows, long long outs, long long ins) {
+  return size_ok(rows, outs) && size_ok(rows, ins) && rows <= FA_MAX_TOKENS && outs * ins <= (1LL << 40);
+}
 size_t layer_norm_ws(long long rows, long long cols, size_t* stats_at) {
   const size_t partials = ws_round(layer_norm_partials_bytes(rows, cols));
   if (stats_at) *stats_at = partials;
@@ -159,7 +163,7 @@ int fa_layer_norm_backward(const void* dy, long long lddy, const void* x, long l
 }
 
 int fa_linear_weight_grad_workspace_bytes(long long rows, long long outs, long long ins, int dtype, size_t* bytes) {
-  if (!bytes || !fa::type_ok(dtype) || !fa::size_ok(rows, outs) || !fa::size_ok(rows, ins)) return FA_ERR_ARG;
+  if (!bytes || !fa::type_ok(dtype) || !fa::product_ok(rows, outs, ins)) return FA_ERR_ARG;
   *bytes = fa::weight_grad_ws(rows, outs, ins, dtype, nullptr);
   return FA_OK;
 }
@@ -167,7 +171,7 @@ int fa_linear_weight_grad_workspace_bytes(long long rows, long long outs, long l
 int fa_linear_weight_grad(const void* dy, long long lddy, int dtype, long long rows, long long outs, const void* ck,
                           long long ins, void* dweight, void* dbias, int gdtype, void* ws, size_t ws_bytes,
                           void* stream) {
-  if (!fa::type_ok(dtype) || !fa::type_ok(gdtype) || !fa::size_ok(rows, outs) || !fa::size_ok(rows, ins) ||
+  if (!fa::type_ok(dtype) || !fa::type_ok(gdtype) || !fa::product_ok(rows, outs, ins) ||
       !fa::in_ok(dy, lddy, rows) || !dweight || !ws || (rows > 0 && !ck))
     return FA_ERR_ARG;
   if (!fa::at(dy, fa::size_of(dtype)) || !fa::at(ck, 16) || !fa::at(dweight, fa::size_of(gdtype)) ||

@@ -1,78 +1,489 @@
 // Weight gradient of a linear layer from the 8-bit checkpoint of its input:
 //   dW[o][i] = sum over tokens t of dY[t][o] * X[t][i],   X read back from the checkpoint.
+//
+// A product of two matrices that are both stored with the summed index (t) as their rows, so both are
+// operands with the kept index contiguous ("MN-major").  The transposed product is formed,
+// D[i][o] = X^T dY, in tiles of 128 inputs x N outputs, on the 5th-generation tensor cores:
+//   * the codes are the operand that needs work before it can be multiplied, so they take the short
+//     side of the tile: converter warps read 64 tokens x 128 codes with plain 16-byte loads, form
+//     code * 2^e in bf16 (exact) and write the 128-byte-swizzled layout the MMA reads;
+//   * dY is loaded by TMA straight into that layout;
+//   * a row of the accumulator is one input, so the 32 lanes of a read-out warp hold 32 neighbouring
+//     inputs of one output: stores to dW are coalesced for any alignment of dW.
+// fp32 dY is split into three bf16 terms (8 + 8 + 8 bits, exact) by a pass in front, and the tile is
+// multiplied with each; the same pass lays out a bf16 dY whose rows TMA cannot address.
+// Few tiles and many tokens: the tokens are split over the blocks, partial products go to scratch in
+// fp32 and a second kernel adds them in a fixed order.
+#include <cuda.h>
+
 #include "../../include/fa.h"
 #include "fa_columns.cuh"
+#include "fa_common.cuh"
+#include "fa_tensor_map.cuh"
 #include "fa_train.h"
 
 namespace fa {
 namespace wgrad {
 
-constexpr int kTile = 64, kTokens = 16;
+constexpr int kTokens = 64;                          // tokens per stage
+constexpr int kIns = 128;                            // inputs per tile: rows of the accumulator
+constexpr int kBoxBytes = 64 * kTokens * 2;          // 64 columns x 64 tokens of bf16
+constexpr int kStageA = 2 * kBoxBytes;
+constexpr int kStagesA = 4;
+constexpr int kConvWarps = 8;
+constexpr int kThreads = 32 * (6 + kConvWarps);      // warp 0 TMA, 1 MMA, 2-5 read-out, 6.. converters
+constexpr int kDepth = 3;                            // stages of codes in flight per converter thread
 
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) simple_kernel(const T* __restrict__ dy, long long lddy, Act8 ck, long long rows,
-                                                     int outs, int ins, int groups, int scale_pitch, void* dw,
-                                                     int gbf16) {
-  __shared__ float a[kTokens][kTile], b[kTokens][kTile];
-  const int o0 = blockIdx.y * kTile, i0 = blockIdx.x * kTile;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float acc[4][4] = {};
-  const int half = threadIdx.x >> 7, k = (threadIdx.x & 127) >> 3, c = threadIdx.x & 7;
-  for (long long t0 = 0; t0 < rows; t0 += kTokens) {
-    const long long t = t0 + k;
-    float v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = 0.f;
-    if (half == 0) {
-      if (t < rows && o0 + c * 8 < outs) load_chunk<T, VEC>(dy + t * lddy, o0 / 8 + c, outs).get(v);
-    } else if (t < rows && i0 + c * 8 < groups * 32) {
-      act8_decode(*reinterpret_cast<const uint2*>(ck.codes + (size_t)t * groups * 32 + i0 + c * 8),
-                  ck.scales[(size_t)t * scale_pitch + (i0 + c * 8) / 32], v);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 8; ++j) (half ? b : a)[k][c * 8 + j] = v[j];
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < kTokens; ++q)
-#pragma unroll
-      for (int y = 0; y < 4; ++y)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) acc[y][x] = fmaf(a[q][ty * 4 + y], b[q][tx + 16 * x], acc[y][x]);
+template <int N> struct Cfg {
+  static constexpr int kStageB = N / 64 * kBoxBytes;
+  static constexpr int kStagesB = N == 256 ? 5 : 8;
+  static constexpr size_t kSmem = 1024 + (size_t)kStagesB * kStageB + (size_t)kStagesA * kStageA + 256;
+  // kind::f16: D fp32, A and B bf16, both MN-major, M = 128
+  static constexpr uint32_t kIdesc =
+      (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(N >> 3) << 17) | ((128u >> 4) << 24);
+};
+
+struct Params {
+  const uint8_t* codes;
+  const uint8_t* scales;
+  long long rows;
+  int groups, scale_pitch;
+  int outs, ins;
+  int planes;                    // terms of dY
+  int tiles_i, tiles;            // tiles along the inputs, in all
+  int splits;
+  int ksteps;                    // stages of tokens in all
+  void* dw;                      // splits == 1
+  int gbf16;
+  float* partials;               // splits > 1: [splits][split_stride]
+  size_t split_stride;
+};
+
+template <int N>
+struct Bars {
+  uint64_t b_full[Cfg<N>::kStagesB], b_empty[Cfg<N>::kStagesB];
+  uint64_t a_full[kStagesA], a_empty[kStagesA];
+  uint64_t acc_full[2], acc_empty[2];
+  uint64_t drained;
+  uint32_t tmem_base;
+  int abort;
+};
+
+// MN-major, 128-byte swizzle: 64 elements x 8 tokens are 1024 bytes; the next 8 tokens follow at once,
+// the next 64 elements a box later.  Descriptor version 1, layout type 2.
+__device__ __forceinline__ uint64_t mn_desc(uint32_t saddr) {
+  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(kBoxBytes >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
+         ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+
+__device__ __forceinline__ void umma(uint32_t tmem_d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void umma_commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
+               : "memory");
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
+        "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
+        "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+      : "memory");
+}
+
+// A unit of work: one tile and one share of the tokens.  Units of one share are neighbours, so the
+// blocks that run at the same time read the same tokens.
+struct Unit {
+  int i0, o0, split, k0, k1;
+};
+__device__ __forceinline__ Unit unit_of(const Params& p, int u, int n) {
+  Unit w;
+  w.split = u / p.tiles;
+  const int tile = u - w.split * p.tiles;
+  const int oi = tile / p.tiles_i;
+  w.i0 = (tile - oi * p.tiles_i) * kIns;
+  w.o0 = oi * n;
+  w.k0 = (int)((long long)p.ksteps * w.split / p.splits);
+  w.k1 = (int)((long long)p.ksteps * (w.split + 1) / p.splits);
+  return w;
+}
+
+// Two codes (bytes 0 and 1 of each half of `x`, spread to 16 bits) times the scale, in bf16: with the
+// code's low 7 bits l and its sign s, (128 + l) - (128 + 128 s) = code; both operands are bf16 by their bits.
+__device__ __forceinline__ uint32_t codes_to_bf16(uint32_t x, __nv_bfloat162 scale) {
+  uint32_t a = (x & 0x007F007Fu) | 0x43004300u, b = (x & 0x00800080u) | 0x43004300u;
+  __nv_bfloat162 v = __hmul2(__hsub2(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b)), scale);
+  return *reinterpret_cast<uint32_t*>(&v);
+}
+__device__ __forceinline__ __nv_bfloat162 scale_bf16(uint32_t byte) {
+  uint32_t s = byte == 255u ? 0x7FC0u : byte == 0u ? 0x0040u : byte << 7;
+  s |= s << 16;
+  return *reinterpret_cast<__nv_bfloat162*>(&s);
+}
+
+template <int N>
+__global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_constant__ CUtensorMap map_dy, Params prm) {
+  using C = Cfg<N>;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* stages_b =
+      reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  unsigned char* stages_a = stages_b + (size_t)C::kStagesB * C::kStageB;
+  Bars<N>* bars = reinterpret_cast<Bars<N>*>(stages_a + (size_t)kStagesA * kStageA);
+  static_assert(sizeof(Bars<N>) <= 256, "barrier block");
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int units = prm.tiles * prm.splits;
+
+  if (tid == 0) {
+    for (int s = 0; s < C::kStagesB; ++s) { mbar_init(&bars->b_full[s], 1); mbar_init(&bars->b_empty[s], 1); }
+    for (int s = 0; s < kStagesA; ++s) { mbar_init(&bars->a_full[s], kConvWarps); mbar_init(&bars->a_empty[s], 1); }
+    for (int s = 0; s < 2; ++s) { mbar_init(&bars->acc_full[s], 1); mbar_init(&bars->acc_empty[s], 4); }
+    mbar_init(&bars->drained, 1);
+    bars->abort = 0;
+    fence_proxy_async();
   }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)),
+                 "r"(2 * N)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t*>(&bars->tmem_base);
+  volatile int* abort = &bars->abort;
+
+  if (warp == 0) {
+    // ---------------- dY tiles by TMA
+    if (lane == 0) {
+      uint32_t n = 0;                                   // stages filled so far
+      bool ok = true;
+      for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
+        const Unit w = unit_of(prm, u, N);
+        for (int k = w.k0; k < w.k1 && ok; ++k)
+          for (int pl = 0; pl < prm.planes; ++pl) {
+            const int s = n % C::kStagesB;
+            if (!mbar_wait(&bars->b_empty[s], ((n / C::kStagesB) & 1) ^ 1) || *abort) { ok = false; break; }
+            mbar_arrive_expect_tx(&bars->b_full[s], C::kStageB);
 #pragma unroll
-  for (int y = 0; y < 4; ++y)
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const int o = o0 + ty * 4 + y, i = i0 + tx + 16 * x;
-      if (o >= outs || i >= ins) continue;
-      const size_t at = (size_t)o * ins + i;
-      if (gbf16) static_cast<bf16*>(dw)[at] = __float2bfloat16_rn(acc[y][x]);
-      else static_cast<float*>(dw)[at] = acc[y][x];
+            for (int q = 0; q < N / 64; ++q)
+              tma_load_3d(stages_b + (size_t)s * C::kStageB + q * kBoxBytes, &map_dy, w.o0 + q * 64, k * kTokens, pl,
+                          &bars->b_full[s]);
+            ++n;
+          }
+      }
+      if (!ok) *abort = 1;
+      // copies still in flight must land before the block may exit
+      const uint32_t first = n > (uint32_t)C::kStagesB ? n - C::kStagesB : 0;
+      for (uint32_t m = first; m < n; ++m) (void)mbar_wait(&bars->b_full[m % C::kStagesB], (m / C::kStagesB) & 1);
     }
+  } else if (warp == 1) {
+    // ---------------- MMA: one thread
+    if (lane == 0) {
+      uint32_t na = 0, nb = 0, nu = 0;
+      bool ok = true;
+      for (int u = blockIdx.x; u < units && ok; u += gridDim.x, ++nu) {
+        const Unit w = unit_of(prm, u, N);
+        const uint32_t acc = nu & 1, d = tmem_base + acc * N;
+        if (!mbar_wait(&bars->acc_empty[acc], ((nu >> 1) & 1) ^ 1) || *abort) { ok = false; break; }
+        for (int k = w.k0; k < w.k1 && ok; ++k, ++na) {
+          const int sa = na % kStagesA;
+          if (!mbar_wait(&bars->a_full[sa], (na / kStagesA) & 1) || *abort) { ok = false; break; }
+          const uint32_t a = smem_u32(stages_a + (size_t)sa * kStageA);
+          for (int pl = 0; pl < prm.planes; ++pl, ++nb) {
+            const int sb = nb % C::kStagesB;
+            if (!mbar_wait(&bars->b_full[sb], (nb / C::kStagesB) & 1) || *abort) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t b = smem_u32(stages_b + (size_t)sb * C::kStageB);
+#pragma unroll
+            for (int q = 0; q < kTokens / 16; ++q)      // 16 tokens are two groups of 8: 2048 bytes
+              umma(d, mn_desc(a + q * 2048), mn_desc(b + q * 2048), C::kIdesc, (k == w.k0 && pl == 0 && q == 0) ? 0u : 1u);
+            umma_commit(&bars->b_empty[sb]);
+          }
+          if (ok) umma_commit(&bars->a_empty[sa]);
+        }
+        if (ok) umma_commit(&bars->acc_full[acc]);
+      }
+      if (!ok) {                                        // products under way must end before the block may exit
+        *abort = 1;
+        umma_commit(&bars->drained);
+        (void)mbar_wait(&bars->drained, 0);
+      }
+    }
+  } else if (warp < 6) {
+    // ---------------- read-out: warp w reads the 32 accumulator rows of its quarter
+    const int quarter = warp & 3;
+    uint32_t nu = 0;
+    for (int u = blockIdx.x; u < units; u += gridDim.x, ++nu) {
+      const Unit w = unit_of(prm, u, N);
+      const uint32_t acc = nu & 1;
+      bool ok = !*abort && mbar_wait(&bars->acc_full[acc], (nu >> 1) & 1) && !*abort;
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok && lane == 0) *abort = 1;
+      tc_fence_after();
+      const int i = w.i0 + quarter * 32 + lane;
+      float* part = prm.partials + (size_t)w.split * prm.split_stride;
+      for (int c = 0; c < N; c += 32) {
+        uint32_t v[32];
+        if (ok) {
+          tmem_ld32(tmem_base + (static_cast<uint32_t>(32 * quarter) << 16) + acc * N + c, v);
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        } else {                                       // a wait ran out: the result shows it
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = 0x7FC00000u;
+        }
+        if (i < prm.ins) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            const int o = w.o0 + c + j;
+            if (o >= prm.outs) break;
+            const size_t at = (size_t)o * prm.ins + i;
+            const float f = __uint_as_float(v[j]);
+            if (prm.splits > 1) part[at] = f;
+            else if (prm.gbf16) static_cast<bf16*>(prm.dw)[at] = __float2bfloat16_rn(f);
+            else static_cast<float*>(prm.dw)[at] = f;
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars->acc_empty[acc]);
+    }
+  } else {
+    // ---------------- converters: thread -> 16 codes of token (t, t + 32) of the stage
+    const int ct = tid - 192, c = ct & 7, t = ct >> 3;
+    int total = 0;
+    for (int u = blockIdx.x; u < units; u += gridDim.x) {
+      const Unit w = unit_of(prm, u, N);
+      total += w.k1 - w.k0;
+    }
+    // the loads run kDepth stages ahead of the conversion
+    int lu = blockIdx.x;
+    Unit lw = unit_of(prm, lu < units ? lu : 0, N);
+    int lk = lw.k0;
+    uint4 q[kDepth][2];
+    uint32_t e[kDepth][2];
+    auto load = [&](uint4 (&dst)[2], uint32_t (&byte)[2]) {
+      const int i = lw.i0 + c * 16;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const long long row = (long long)lk * kTokens + t + h * 32;
+        if (row < prm.rows && i < prm.groups * 32) {
+          dst[h] = __ldg(reinterpret_cast<const uint4*>(prm.codes + (size_t)row * prm.groups * 32 + i));
+          byte[h] = __ldg(prm.scales + (size_t)row * prm.scale_pitch + (i >> 5));
+        } else {
+          dst[h] = make_uint4(0, 0, 0, 0);
+          byte[h] = 127;
+        }
+      }
+      if (++lk == lw.k1) {
+        lu += gridDim.x;
+        if (lu < units) { lw = unit_of(prm, lu, N); lk = lw.k0; }
+      }
+    };
+#pragma unroll
+    for (int j = 0; j < kDepth; ++j)
+      if (j < total) load(q[j], e[j]);
+    bool ok = true;
+    for (int n0 = 0; n0 < total && ok; n0 += kDepth) {
+#pragma unroll
+      for (int j = 0; j < kDepth; ++j) {
+        const int n = n0 + j;
+        if (n >= total || !ok) continue;
+        const int s = n % kStagesA;
+        ok = mbar_wait(&bars->a_empty[s], ((n / kStagesA) & 1) ^ 1) && !*abort;
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) continue;
+        unsigned char* base = stages_a + (size_t)s * kStageA + (c >> 2) * kBoxBytes;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const __nv_bfloat162 sc = scale_bf16(e[j][h]);
+          const uint4 x = q[j][h];
+          uint4 lo, hi;
+          lo.x = codes_to_bf16(__byte_perm(x.x, 0, 0x4140), sc); lo.y = codes_to_bf16(__byte_perm(x.x, 0, 0x4342), sc);
+          lo.z = codes_to_bf16(__byte_perm(x.y, 0, 0x4140), sc); lo.w = codes_to_bf16(__byte_perm(x.y, 0, 0x4342), sc);
+          hi.x = codes_to_bf16(__byte_perm(x.z, 0, 0x4140), sc); hi.y = codes_to_bf16(__byte_perm(x.z, 0, 0x4342), sc);
+          hi.z = codes_to_bf16(__byte_perm(x.w, 0, 0x4140), sc); hi.w = codes_to_bf16(__byte_perm(x.w, 0, 0x4342), sc);
+          const int tt = t + h * 32;
+          unsigned char* row = base + tt * 128;
+          const int ch = (c & 3) * 2, swap = c >> 2;     // the upper half stores its odd chunk first: no two lanes on a bank
+          *reinterpret_cast<uint4*>(row + (((ch + swap) ^ (tt & 7)) << 4)) = swap ? hi : lo;
+          *reinterpret_cast<uint4*>(row + (((ch + 1 - swap) ^ (tt & 7)) << 4)) = swap ? lo : hi;
+        }
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars->a_full[s]);
+        if (n + kDepth < total) load(q[j], e[j]);
+      }
+    }
+    if (!ok && lane == 0) *abort = 1;
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(2 * N) : "memory");
+  }
+}
+
+// out[j] = sum of the partial products, in order.
+__global__ void __launch_bounds__(256) add_splits_kernel(const float* __restrict__ partials, size_t split_stride,
+                                                         int splits, size_t n, void* out, int gbf16) {
+  const size_t j = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (j >= n) return;
+  float v = 0.f;
+#pragma unroll 8
+  for (int s = 0; s < splits; ++s) v += partials[s * split_stride + j];
+  if (gbf16) static_cast<bf16*>(out)[j] = __float2bfloat16_rn(v);
+  else static_cast<float*>(out)[j] = v;
+}
+
+// dY as bf16 terms that add up to it exactly, rows of `pitch` elements: [planes][rows][pitch].  Terms are
+// cut off rather than rounded, so that no finite value becomes infinite; what is not finite is one term.
+template <typename T>
+__global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ dy, long long ld, long long rows, int outs,
+                                                   int pitch, int planes, bf16* __restrict__ out) {
+  const int chunks = pitch / 8;
+  const long long n = rows * chunks, plane = rows * pitch;
+  for (long long j = (long long)blockIdx.x * 256 + threadIdx.x; j < n; j += (long long)gridDim.x * 256) {
+    const long long r = j / chunks;
+    const int c = static_cast<int>(j - r * chunks);
+    float v[8];
+    load_chunk<T, false>(dy + r * ld, c, outs).get(v);
+    for (int p = 0; p < planes; ++p) {
+      float term[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        term[k] = sizeof(T) == 2 ? v[k] : __uint_as_float(__float_as_uint(v[k]) & 0xffff0000u);
+        if (isnan(v[k])) term[k] = v[k];
+        v[k] = isfinite(v[k]) ? v[k] - term[k] : 0.f;
+      }
+      Raw8<bf16> o;
+      o.put(term);
+      o.store(out + p * plane + r * pitch + c * 8);
+    }
+  }
+}
+
+// How a product is cut up.  Per block and stage the MMA takes N / 256 * 512 cycles or so; a split costs
+// a write and a read of the whole result.
+struct Plan {
+  int n, tiles_i, tiles_o, tiles, splits, ksteps, planes;
+  bool pack;
+  int pitch;
+  size_t pack_bytes, split_stride;
+};
+
+Plan plan_of(long long rows, long long outs, long long ins, int dtype, bool pack) {
+  Plan p{};
+  p.planes = dtype == FA_F32 ? 3 : 1;
+  p.pack = pack;
+  p.pitch = static_cast<int>((outs + 7) / 8 * 8);
+  p.pack_bytes = pack ? ((size_t)p.planes * rows * p.pitch * 2 + 255) / 256 * 256 : 0;
+  p.n = outs <= 128 ? 128 : 256;
+  p.tiles_i = static_cast<int>((ins + kIns - 1) / kIns);
+  p.tiles_o = static_cast<int>((outs + p.n - 1) / p.n);
+  p.ksteps = static_cast<int>((rows + kTokens - 1) / kTokens);
+  const long long tiles = (long long)p.tiles_i * p.tiles_o;
+  p.tiles = static_cast<int>(tiles);
+  const int sms = sm_count();
+  // splits that fill the blocks once; each keeps at least 4 stages
+  long long s = tiles >= sms ? 1 : sms / tiles;
+  if (s > (p.ksteps + 3) / 4) s = (p.ksteps + 3) / 4;
+  if (s > 32) s = 32;
+  p.splits = static_cast<int>(s < 1 ? 1 : s);
+  p.split_stride = ((size_t)outs * ins + 63) / 64 * 64;
+  return p;
 }
 
 }  // namespace wgrad
 
-size_t linear_weight_grad_scratch_bytes(long long, long long, long long, int) { return 0; }
+size_t linear_weight_grad_scratch_bytes(long long rows, long long outs, long long ins, int dtype) {
+  const wgrad::Plan p = wgrad::plan_of(rows, outs, ins, dtype, true);   // whether dY has to be laid out is known at the call
+  return p.pack_bytes + (p.splits > 1 ? p.splits * p.split_stride * sizeof(float) : 0);
+}
 
-template <typename T>
-static cudaError_t weight_grad_t(Mat dy, long long rows, long long outs, long long ins, const void* ck, void* dweight,
-                                 int gdtype, cudaStream_t st) {
-  const dim3 grid((ins + wgrad::kTile - 1) / wgrad::kTile, (outs + wgrad::kTile - 1) / wgrad::kTile);
-  auto go = [&](auto kernel) {
-    kernel<<<grid, 256, 0, st>>>(row_of<T>(dy, 0), dy.ld, act8_at(ck, rows, ins, 0), rows, (int)outs, (int)ins,
-                                 (int)act8_groups(ins), (int)act8_scale_pitch(ins), dweight, gdtype == FA_BF16);
-  };
-  if (mat_vec<T>(dy, outs)) go(wgrad::simple_kernel<T, true>);
-  else go(wgrad::simple_kernel<T, false>);
+template <int N>
+static cudaError_t launch_product(const CUtensorMap& map, const wgrad::Params& prm, cudaStream_t st) {
+  using C = wgrad::Cfg<N>;
+  cudaError_t e = cudaFuncSetAttribute(wgrad::weight_grad_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       static_cast<int>(C::kSmem));
+  if (e != cudaSuccess) return e;
+  const int units = prm.tiles * prm.splits, sms = sm_count();
+  wgrad::weight_grad_kernel<N><<<units < sms ? units : sms, wgrad::kThreads, C::kSmem, st>>>(map, prm);
   return cudaGetLastError();
 }
 
 cudaError_t launch_linear_weight_grad(Mat dy, int dtype, long long rows, long long outs, long long ins, const void* ck,
-                                      void* dweight, int gdtype, void*, cudaStream_t st) {
-  return dtype == FA_BF16 ? weight_grad_t<bf16>(dy, rows, outs, ins, ck, dweight, gdtype, st)
-                          : weight_grad_t<float>(dy, rows, outs, ins, ck, dweight, gdtype, st);
+                                      void* dweight, int gdtype, void* scratch, cudaStream_t st) {
+  const size_t n = (size_t)outs * ins;
+  if (rows == 0) return cudaMemsetAsync(dweight, 0, n * (gdtype == FA_BF16 ? 2 : 4), st);
+  const bool direct = dtype == FA_BF16 && aligned16(dy.p) && dy.ld % 8 == 0 && dy.ld >= outs && dy.ld < (1LL << 38);
+  const wgrad::Plan p = wgrad::plan_of(rows, outs, ins, dtype, !direct);
+  const void* base = dy.p;
+  long long ld = dy.ld;
+  if (!direct) {
+    bf16* packed = static_cast<bf16*>(scratch);
+    const long long chunks = rows * (p.pitch / 8);
+    const long long want = (chunks + 255) / 256, most = 16LL * sm_count();
+    const unsigned grid = static_cast<unsigned>(want < most ? want : most);
+    if (dtype == FA_BF16)
+      wgrad::pack_kernel<bf16><<<grid, 256, 0, st>>>(row_of<bf16>(dy, 0), dy.ld, rows, (int)outs, p.pitch, p.planes, packed);
+    else
+      wgrad::pack_kernel<float><<<grid, 256, 0, st>>>(row_of<float>(dy, 0), dy.ld, rows, (int)outs, p.pitch, p.planes, packed);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    base = packed;
+    ld = p.pitch;
+  }
+  EncodeTiledFn enc = encode_tiled();
+  if (!enc) return cudaErrorNotSupported;
+  CUtensorMap map;
+  const cuuint64_t dims[3] = {(cuuint64_t)outs, (cuuint64_t)rows, (cuuint64_t)p.planes};
+  const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (p.planes > 1 ? rows : 1)};
+  const cuuint32_t box[3] = {64, wgrad::kTokens, 1};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  if (enc(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return cudaErrorInvalidValue;
+  const Act8 a = act8_at(ck, rows, ins, 0);
+  wgrad::Params prm{};
+  prm.codes = a.codes; prm.scales = a.scales;
+  prm.rows = rows;
+  prm.groups = static_cast<int>(act8_groups(ins));
+  prm.scale_pitch = static_cast<int>(act8_scale_pitch(ins));
+  prm.outs = static_cast<int>(outs); prm.ins = static_cast<int>(ins);
+  prm.planes = p.planes;
+  prm.tiles_i = p.tiles_i; prm.tiles = p.tiles; prm.splits = p.splits; prm.ksteps = p.ksteps;
+  prm.dw = dweight; prm.gbf16 = gdtype == FA_BF16;
+  prm.partials = reinterpret_cast<float*>(static_cast<char*>(scratch) + p.pack_bytes);
+  prm.split_stride = p.split_stride;
+  cudaError_t e = p.n == 256 ? launch_product<256>(map, prm, st) : launch_product<128>(map, prm, st);
+  if (e != cudaSuccess || p.splits == 1) return e;
+  wgrad::add_splits_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(prm.partials, p.split_stride, p.splits, n, dweight,
+                                                                       prm.gbf16);
+  return cudaGetLastError();
 }
 
 }  // namespace fa
