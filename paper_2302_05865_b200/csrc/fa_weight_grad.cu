@@ -5,8 +5,10 @@
 // operands with the kept index contiguous ("MN-major").  The transposed product is formed,
 // D[i][o] = X^T dY, in tiles of 128 inputs x N outputs, on the 5th-generation tensor cores:
 //   * the codes are the operand that needs work before it can be multiplied, so they take the short
-//     side of the tile: converter warps read 64 tokens x 128 codes with plain 16-byte loads, form
-//     code * 2^e in bf16 (exact) and write the 128-byte-swizzled layout the MMA reads;
+//     side of the tile: 64 tokens x 128 codes come in by TMA, their scales by 4-byte asynchronous
+//     copies, and converter warps form code * 2^e in bf16 (exact) and write the 128-byte-swizzled layout
+//     the MMA reads.  (Loads from global memory in these warps, three or four stages ahead in
+//     registers, were waited for all the same: twice the time of the products);
 //   * dY is loaded by TMA straight into that layout;
 //   * a row of the accumulator is one input, so the 32 lanes of a read-out warp hold 32 neighbouring
 //     inputs of one output: stores to dW are coalesced for any alignment of dW.
@@ -29,25 +31,28 @@ constexpr int kTokens = 64;                          // tokens per stage
 constexpr int kIns = 128;                            // inputs per tile: rows of the accumulator
 constexpr int kBoxBytes = 64 * kTokens * 2;          // 64 columns x 64 tokens of bf16
 constexpr int kStageA = 2 * kBoxBytes;
-constexpr int kStagesA = 4;
-constexpr int kConvWarps = 8;
-constexpr int kThreads = 32 * (6 + kConvWarps);      // warp 0 TMA, 1 MMA, 2-5 read-out, 6.. converters
-constexpr int kDepth = 3;                            // stages of codes in flight per converter thread
+constexpr int kStagesA = 3;
+constexpr int kCodeBytes = kIns * kTokens;           // codes of a stage as they are stored
+constexpr int kRawBytes = kCodeBytes + 4 * kTokens;  // and the scales of the tile's four groups, a word per token
+constexpr int kStagesRaw = 4;
+constexpr int kConvGroups = 2;                       // a group of four warps converts every second stage
+constexpr int kScaleWarp = 6 + 4 * kConvGroups;
+constexpr int kThreads = 32 * (kScaleWarp + 1);      // warp 0 TMA, 1 MMA, 2-5 read-out, 6.. converters, last scales
 
 template <int N> struct Cfg {
   static constexpr int kStageB = N / 64 * kBoxBytes;
-  static constexpr int kStagesB = N == 256 ? 5 : 8;
-  static constexpr size_t kSmem = 1024 + (size_t)kStagesB * kStageB + (size_t)kStagesA * kStageA + 256;
+  static constexpr int kStagesB = N == 256 ? 4 : 6;
+  static constexpr size_t kSmem = 1024 + (size_t)kStagesB * kStageB + (size_t)kStagesA * kStageA +
+                                  (size_t)kStagesRaw * kRawBytes + 256;
   // kind::f16: D fp32, A and B bf16, both MN-major, M = 128
   static constexpr uint32_t kIdesc =
       (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(N >> 3) << 17) | ((128u >> 4) << 24);
 };
 
 struct Params {
-  const uint8_t* codes;
   const uint8_t* scales;
   long long rows;
-  int groups, scale_pitch;
+  int scale_pitch;
   int outs, ins;
   int planes;                    // terms of dY
   int tiles_i, tiles;            // tiles along the inputs, in all
@@ -63,6 +68,7 @@ template <int N>
 struct Bars {
   uint64_t b_full[Cfg<N>::kStagesB], b_empty[Cfg<N>::kStagesB];
   uint64_t a_full[kStagesA], a_empty[kStagesA];
+  uint64_t raw_full[kStagesRaw], raw_empty[kStagesRaw];
   uint64_t acc_full[2], acc_empty[2];
   uint64_t drained;
   uint32_t tmem_base;
@@ -141,20 +147,23 @@ __device__ __forceinline__ __nv_bfloat162 scale_bf16(uint32_t byte) {
 }
 
 template <int N>
-__global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_constant__ CUtensorMap map_dy, Params prm) {
+__global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_constant__ CUtensorMap map_dy,
+                                                                  const __grid_constant__ CUtensorMap map_codes, Params prm) {
   using C = Cfg<N>;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* stages_b =
       reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   unsigned char* stages_a = stages_b + (size_t)C::kStagesB * C::kStageB;
-  Bars<N>* bars = reinterpret_cast<Bars<N>*>(stages_a + (size_t)kStagesA * kStageA);
+  unsigned char* raws = stages_a + (size_t)kStagesA * kStageA;
+  Bars<N>* bars = reinterpret_cast<Bars<N>*>(raws + (size_t)kStagesRaw * kRawBytes);
   static_assert(sizeof(Bars<N>) <= 256, "barrier block");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int units = prm.tiles * prm.splits;
 
   if (tid == 0) {
     for (int s = 0; s < C::kStagesB; ++s) { mbar_init(&bars->b_full[s], 1); mbar_init(&bars->b_empty[s], 1); }
-    for (int s = 0; s < kStagesA; ++s) { mbar_init(&bars->a_full[s], kConvWarps); mbar_init(&bars->a_empty[s], 1); }
+    for (int s = 0; s < kStagesA; ++s) { mbar_init(&bars->a_full[s], 4); mbar_init(&bars->a_empty[s], 1); }
+    for (int s = 0; s < kStagesRaw; ++s) { mbar_init(&bars->raw_full[s], 1 + 32); mbar_init(&bars->raw_empty[s], 4); }
     for (int s = 0; s < 2; ++s) { mbar_init(&bars->acc_full[s], 1); mbar_init(&bars->acc_empty[s], 4); }
     mbar_init(&bars->drained, 1);
     bars->abort = 0;
@@ -173,13 +182,18 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
   volatile int* abort = &bars->abort;
 
   if (warp == 0) {
-    // ---------------- dY tiles by TMA
+    // ---------------- codes and dY by TMA
     if (lane == 0) {
-      uint32_t n = 0;                                   // stages filled so far
+      uint32_t n = 0, nr = 0;                           // stages of dY and of codes asked for so far
       bool ok = true;
       for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
         const Unit w = unit_of(prm, u, N);
-        for (int k = w.k0; k < w.k1 && ok; ++k)
+        for (int k = w.k0; k < w.k1 && ok; ++k) {
+          const int r = nr % kStagesRaw;
+          if (!mbar_wait(&bars->raw_empty[r], ((nr / kStagesRaw) & 1) ^ 1) || *abort) { ok = false; break; }
+          mbar_arrive_expect_tx(&bars->raw_full[r], kCodeBytes);
+          tma_load_2d(raws + (size_t)r * kRawBytes, &map_codes, w.i0, k * kTokens, &bars->raw_full[r]);
+          ++nr;
           for (int pl = 0; pl < prm.planes; ++pl) {
             const int s = n % C::kStagesB;
             if (!mbar_wait(&bars->b_empty[s], ((n / C::kStagesB) & 1) ^ 1) || *abort) { ok = false; break; }
@@ -190,45 +204,54 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
                           &bars->b_full[s]);
             ++n;
           }
+        }
       }
       if (!ok) *abort = 1;
       // copies still in flight must land before the block may exit
-      const uint32_t first = n > (uint32_t)C::kStagesB ? n - C::kStagesB : 0;
-      for (uint32_t m = first; m < n; ++m) (void)mbar_wait(&bars->b_full[m % C::kStagesB], (m / C::kStagesB) & 1);
+      for (uint32_t m = n > (uint32_t)C::kStagesB ? n - C::kStagesB : 0; m < n; ++m)
+        (void)mbar_wait(&bars->b_full[m % C::kStagesB], (m / C::kStagesB) & 1);
+      for (uint32_t m = nr > (uint32_t)kStagesRaw ? nr - kStagesRaw : 0; m < nr; ++m)
+        (void)mbar_wait(&bars->raw_full[m % kStagesRaw], (m / kStagesRaw) & 1);
     }
   } else if (warp == 1) {
-    // ---------------- MMA: one thread
-    if (lane == 0) {
-      uint32_t na = 0, nb = 0, nu = 0;
-      bool ok = true;
-      for (int u = blockIdx.x; u < units && ok; u += gridDim.x, ++nu) {
-        const Unit w = unit_of(prm, u, N);
-        const uint32_t acc = nu & 1, d = tmem_base + acc * N;
-        if (!mbar_wait(&bars->acc_empty[acc], ((nu >> 1) & 1) ^ 1) || *abort) { ok = false; break; }
-        for (int k = w.k0; k < w.k1 && ok; ++k, ++na) {
-          const int sa = na % kStagesA;
-          if (!mbar_wait(&bars->a_full[sa], (na / kStagesA) & 1) || *abort) { ok = false; break; }
-          const uint32_t a = smem_u32(stages_a + (size_t)sa * kStageA);
-          for (int pl = 0; pl < prm.planes; ++pl, ++nb) {
-            const int sb = nb % C::kStagesB;
-            if (!mbar_wait(&bars->b_full[sb], (nb / C::kStagesB) & 1) || *abort) { ok = false; break; }
-            tc_fence_after();
-            const uint32_t b = smem_u32(stages_b + (size_t)sb * C::kStageB);
+    // ---------------- MMA: the warp waits together, one elected thread issues.  (With the whole role in an
+    // `if (lane == 0)` the products alone took a fifth longer: 579 against 484 us for 16384 x 4096 x 4096.)
+    uint32_t leader;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(leader));
+    uint32_t na = 0, nb = 0, nu = 0;
+    bool ok = true;
+    for (int u = blockIdx.x; u < units && ok; u += gridDim.x, ++nu) {
+      const Unit w = unit_of(prm, u, N);
+      const uint32_t acc = nu & 1, d = tmem_base + acc * N;
+      ok = __all_sync(0xffffffffu, mbar_wait(&bars->acc_empty[acc], ((nu >> 1) & 1) ^ 1) && !*abort);
+      for (int k = w.k0; k < w.k1 && ok; ++k, ++na) {
+        const int sa = na % kStagesA;
+        ok = __all_sync(0xffffffffu, mbar_wait(&bars->a_full[sa], (na / kStagesA) & 1) && !*abort);
+        const uint32_t a = smem_u32(stages_a + (size_t)sa * kStageA);
+        for (int pl = 0; pl < prm.planes && ok; ++pl, ++nb) {
+          const int sb = nb % C::kStagesB;
+          ok = __all_sync(0xffffffffu, mbar_wait(&bars->b_full[sb], (nb / C::kStagesB) & 1) && !*abort);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t b = smem_u32(stages_b + (size_t)sb * C::kStageB);
+          if (leader) {
 #pragma unroll
             for (int q = 0; q < kTokens / 16; ++q)      // 16 tokens are two groups of 8: 2048 bytes
               umma(d, mn_desc(a + q * 2048), mn_desc(b + q * 2048), C::kIdesc, (k == w.k0 && pl == 0 && q == 0) ? 0u : 1u);
             umma_commit(&bars->b_empty[sb]);
+            if (pl == prm.planes - 1) umma_commit(&bars->a_empty[sa]);
           }
-          if (ok) umma_commit(&bars->a_empty[sa]);
+          __syncwarp();
         }
-        if (ok) umma_commit(&bars->acc_full[acc]);
       }
-      if (!ok) {                                        // products under way must end before the block may exit
-        *abort = 1;
-        umma_commit(&bars->drained);
-        (void)mbar_wait(&bars->drained, 0);
-      }
+      if (ok && leader) umma_commit(&bars->acc_full[acc]);
     }
+    if (!ok && leader) {                                // products under way must end before the block may exit
+      *abort = 1;
+      umma_commit(&bars->drained);
+      (void)mbar_wait(&bars->drained, 0);
+    }
+    __syncwarp();
   } else if (warp < 6) {
     // ---------------- read-out: warp w reads the 32 accumulator rows of its quarter
     const int quarter = warp & 3;
@@ -268,73 +291,79 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
       __syncwarp();
       if (lane == 0) mbar_arrive(&bars->acc_empty[acc]);
     }
-  } else {
-    // ---------------- converters: thread -> 16 codes of token (t, t + 32) of the stage
-    const int ct = tid - 192, c = ct & 7, t = ct >> 3;
+  } else if (warp < kScaleWarp) {
+    // ---------------- converters: thread -> 16 codes of tokens t, t + 16, t + 32, t + 48 of the stage
+    const int ct = (tid - 192) & 127, c = ct & 7, t = ct >> 3;
     int total = 0;
     for (int u = blockIdx.x; u < units; u += gridDim.x) {
       const Unit w = unit_of(prm, u, N);
       total += w.k1 - w.k0;
     }
-    // the loads run kDepth stages ahead of the conversion
-    int lu = blockIdx.x;
-    Unit lw = unit_of(prm, lu < units ? lu : 0, N);
-    int lk = lw.k0;
-    uint4 q[kDepth][2];
-    uint32_t e[kDepth][2];
-    auto load = [&](uint4 (&dst)[2], uint32_t (&byte)[2]) {
-      const int i = lw.i0 + c * 16;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const long long row = (long long)lk * kTokens + t + h * 32;
-        if (row < prm.rows && i < prm.groups * 32) {
-          dst[h] = __ldg(reinterpret_cast<const uint4*>(prm.codes + (size_t)row * prm.groups * 32 + i));
-          byte[h] = __ldg(prm.scales + (size_t)row * prm.scale_pitch + (i >> 5));
-        } else {
-          dst[h] = make_uint4(0, 0, 0, 0);
-          byte[h] = 127;
-        }
-      }
-      if (++lk == lw.k1) {
-        lu += gridDim.x;
-        if (lu < units) { lw = unit_of(prm, lu, N); lk = lw.k0; }
-      }
-    };
-#pragma unroll
-    for (int j = 0; j < kDepth; ++j)
-      if (j < total) load(q[j], e[j]);
     bool ok = true;
-    for (int n0 = 0; n0 < total && ok; n0 += kDepth) {
+    for (int n = (warp - 6) >> 2; n < total; n += kConvGroups) {
+      const int s = n % kStagesA, r = n % kStagesRaw;
+      ok = __all_sync(0xffffffffu, mbar_wait(&bars->raw_full[r], (n / kStagesRaw) & 1) && !*abort);
+      if (!ok) break;
+      const unsigned char* raw = raws + (size_t)r * kRawBytes;
+      uint4 q[4];
+      uint32_t e[4];
 #pragma unroll
-      for (int j = 0; j < kDepth; ++j) {
-        const int n = n0 + j;
-        if (n >= total || !ok) continue;
-        const int s = n % kStagesA;
-        ok = mbar_wait(&bars->a_empty[s], ((n / kStagesA) & 1) ^ 1) && !*abort;
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) continue;
-        unsigned char* base = stages_a + (size_t)s * kStageA + (c >> 2) * kBoxBytes;
+      for (int h = 0; h < 4; ++h) {
+        q[h] = *reinterpret_cast<const uint4*>(raw + (t + h * 16) * kIns + c * 16);
+        e[h] = raw[kCodeBytes + (t + h * 16) * 4 + (c >> 1)];
+      }
+      ok = __all_sync(0xffffffffu, mbar_wait(&bars->a_empty[s], ((n / kStagesA) & 1) ^ 1) && !*abort);
+      if (!ok) break;
+      unsigned char* base = stages_a + (size_t)s * kStageA + (c >> 2) * kBoxBytes;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const __nv_bfloat162 sc = scale_bf16(e[j][h]);
-          const uint4 x = q[j][h];
-          uint4 lo, hi;
-          lo.x = codes_to_bf16(__byte_perm(x.x, 0, 0x4140), sc); lo.y = codes_to_bf16(__byte_perm(x.x, 0, 0x4342), sc);
-          lo.z = codes_to_bf16(__byte_perm(x.y, 0, 0x4140), sc); lo.w = codes_to_bf16(__byte_perm(x.y, 0, 0x4342), sc);
-          hi.x = codes_to_bf16(__byte_perm(x.z, 0, 0x4140), sc); hi.y = codes_to_bf16(__byte_perm(x.z, 0, 0x4342), sc);
-          hi.z = codes_to_bf16(__byte_perm(x.w, 0, 0x4140), sc); hi.w = codes_to_bf16(__byte_perm(x.w, 0, 0x4342), sc);
-          const int tt = t + h * 32;
-          unsigned char* row = base + tt * 128;
-          const int ch = (c & 3) * 2, swap = c >> 2;     // the upper half stores its odd chunk first: no two lanes on a bank
-          *reinterpret_cast<uint4*>(row + (((ch + swap) ^ (tt & 7)) << 4)) = swap ? hi : lo;
-          *reinterpret_cast<uint4*>(row + (((ch + 1 - swap) ^ (tt & 7)) << 4)) = swap ? lo : hi;
-        }
-        fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bars->a_full[s]);
-        if (n + kDepth < total) load(q[j], e[j]);
+      for (int h = 0; h < 4; ++h) {
+        const __nv_bfloat162 sc = scale_bf16(e[h]);
+        const uint4 x = q[h];
+        uint4 lo, hi;
+        lo.x = codes_to_bf16(__byte_perm(x.x, 0, 0x4140), sc); lo.y = codes_to_bf16(__byte_perm(x.x, 0, 0x4342), sc);
+        lo.z = codes_to_bf16(__byte_perm(x.y, 0, 0x4140), sc); lo.w = codes_to_bf16(__byte_perm(x.y, 0, 0x4342), sc);
+        hi.x = codes_to_bf16(__byte_perm(x.z, 0, 0x4140), sc); hi.y = codes_to_bf16(__byte_perm(x.z, 0, 0x4342), sc);
+        hi.z = codes_to_bf16(__byte_perm(x.w, 0, 0x4140), sc); hi.w = codes_to_bf16(__byte_perm(x.w, 0, 0x4342), sc);
+        const int tt = t + h * 16;
+        unsigned char* row = base + tt * 128;
+        const int ch = (c & 3) * 2, swap = c >> 2;       // the upper half stores its odd chunk first: no two lanes on a bank
+        *reinterpret_cast<uint4*>(row + (((ch + swap) ^ (tt & 7)) << 4)) = swap ? hi : lo;
+        *reinterpret_cast<uint4*>(row + (((ch + 1 - swap) ^ (tt & 7)) << 4)) = swap ? lo : hi;
+      }
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(&bars->raw_empty[r]);
+        mbar_arrive(&bars->a_full[s]);
       }
     }
+    if (!ok && lane == 0) *abort = 1;
+  } else {
+    // ---------------- scales: a lane copies the words of two tokens; words past the last token are zero
+    // (their codes are zero as well), the copies' arrival is counted on the stage's barrier
+    uint32_t nr = 0;
+    bool ok = true;
+    for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
+      const Unit w = unit_of(prm, u, N);
+      const uint8_t* column = prm.scales + (w.i0 >> 5);
+      for (int k = w.k0; k < w.k1; ++k, ++nr) {
+        const int r = nr % kStagesRaw;
+        ok = __all_sync(0xffffffffu, mbar_wait(&bars->raw_empty[r], ((nr / kStagesRaw) & 1) ^ 1) && !*abort);
+        if (!ok) break;
+        const uint32_t dst = smem_u32(raws + (size_t)r * kRawBytes + kCodeBytes);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int t = lane + h * 32;
+          const long long row = (long long)k * kTokens + t;
+          const bool inside = row < prm.rows;
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst + t * 4),
+                       "l"(column + (size_t)(inside ? row : 0) * prm.scale_pitch), "r"(inside ? 4 : 0)
+                       : "memory");
+        }
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&bars->raw_full[r])) : "memory");
+      }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");     // nothing of this thread's is in flight at exit
     if (!ok && lane == 0) *abort = 1;
   }
 
@@ -424,13 +453,14 @@ size_t linear_weight_grad_scratch_bytes(long long rows, long long outs, long lon
 }
 
 template <int N>
-static cudaError_t launch_product(const CUtensorMap& map, const wgrad::Params& prm, cudaStream_t st) {
+static cudaError_t launch_product(const CUtensorMap& map, const CUtensorMap& map_codes, const wgrad::Params& prm,
+                                  cudaStream_t st) {
   using C = wgrad::Cfg<N>;
   cudaError_t e = cudaFuncSetAttribute(wgrad::weight_grad_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                        static_cast<int>(C::kSmem));
   if (e != cudaSuccess) return e;
   const int units = prm.tiles * prm.splits, sms = sm_count();
-  wgrad::weight_grad_kernel<N><<<units < sms ? units : sms, wgrad::kThreads, C::kSmem, st>>>(map, prm);
+  wgrad::weight_grad_kernel<N><<<units < sms ? units : sms, wgrad::kThreads, C::kSmem, st>>>(map, map_codes, prm);
   return cudaGetLastError();
 }
 
@@ -468,10 +498,17 @@ cudaError_t launch_linear_weight_grad(Mat dy, int dtype, long long rows, long lo
           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
   const Act8 a = act8_at(ck, rows, ins, 0);
+  CUtensorMap map_codes;
+  const cuuint64_t code_dims[2] = {(cuuint64_t)act8_groups(ins) * 32, (cuuint64_t)rows};
+  const cuuint64_t code_strides[1] = {(cuuint64_t)act8_groups(ins) * 32};
+  const cuuint32_t code_box[2] = {wgrad::kIns, wgrad::kTokens};
+  if (enc(&map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, a.codes, code_dims, code_strides, code_box, estr,
+          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return cudaErrorInvalidValue;
   wgrad::Params prm{};
-  prm.codes = a.codes; prm.scales = a.scales;
+  prm.scales = a.scales;
   prm.rows = rows;
-  prm.groups = static_cast<int>(act8_groups(ins));
   prm.scale_pitch = static_cast<int>(act8_scale_pitch(ins));
   prm.outs = static_cast<int>(outs); prm.ins = static_cast<int>(ins);
   prm.planes = p.planes;
@@ -479,7 +516,7 @@ cudaError_t launch_linear_weight_grad(Mat dy, int dtype, long long rows, long lo
   prm.dw = dweight; prm.gbf16 = gdtype == FA_BF16;
   prm.partials = reinterpret_cast<float*>(static_cast<char*>(scratch) + p.pack_bytes);
   prm.split_stride = p.split_stride;
-  cudaError_t e = p.n == 256 ? launch_product<256>(map, prm, st) : launch_product<128>(map, prm, st);
+  cudaError_t e = p.n == 256 ? launch_product<256>(map, map_codes, prm, st) : launch_product<128>(map, map_codes, prm, st);
   if (e != cudaSuccess || p.splits == 1) return e;
   wgrad::add_splits_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(prm.partials, p.split_stride, p.splits, n, dweight,
                                                                        prm.gbf16);
