@@ -30,20 +30,19 @@ namespace wgrad {
 constexpr int kTokens = 64;                          // tokens per stage
 constexpr int kIns = 128;                            // inputs per tile: rows of the accumulator
 constexpr int kBoxBytes = 64 * kTokens * 2;          // 64 columns x 64 tokens of bf16
-constexpr int kStageA = 2 * kBoxBytes;
-constexpr int kStagesA = 3;
+constexpr int kBytesA = 2 * kBoxBytes;
 constexpr int kCodeBytes = kIns * kTokens;           // codes of a stage as they are stored
 constexpr int kRawBytes = kCodeBytes + 4 * kTokens;  // and the scales of the tile's four groups, a word per token
 constexpr int kStagesRaw = 4;
-constexpr int kConvGroups = 2;                       // a group of four warps converts every second stage
+constexpr int kConvGroups = 3;                       // a group of four warps converts every third stage
 constexpr int kScaleWarp = 6 + 4 * kConvGroups;
 constexpr int kThreads = 32 * (kScaleWarp + 1);      // warp 0 TMA, 1 MMA, 2-5 read-out, 6.. converters, last scales
 
 template <int N> struct Cfg {
-  static constexpr int kStageB = N / 64 * kBoxBytes;
-  static constexpr int kStagesB = N == 256 ? 4 : 6;
-  static constexpr size_t kSmem = 1024 + (size_t)kStagesB * kStageB + (size_t)kStagesA * kStageA +
-                                  (size_t)kStagesRaw * kRawBytes + 256;
+  static constexpr int kBytesB = N / 64 * kBoxBytes;
+  static constexpr int kStage = kBytesA + kBytesB;   // a stage: codes as bf16, then dY
+  static constexpr int kStages = N == 256 ? 4 : 5;
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + (size_t)kStagesRaw * kRawBytes + 256;
   // kind::f16: D fp32, A and B bf16, both MN-major, M = 128
   static constexpr uint32_t kIdesc =
       (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(N >> 3) << 17) | ((128u >> 4) << 24);
@@ -54,10 +53,10 @@ struct Params {
   long long rows;
   int scale_pitch;
   int outs, ins;
-  int planes;                    // terms of dY
+  int planes;                    // terms of dY; every term is a step of its own, with the codes converted anew
   int tiles_i, tiles;            // tiles along the inputs, in all
   int splits;
-  int ksteps;                    // stages of tokens in all
+  int ksteps;                    // steps in all: stages of tokens x terms
   void* dw;                      // splits == 1
   int gbf16;
   float* partials;               // splits > 1: [splits][split_stride]
@@ -66,13 +65,11 @@ struct Params {
 
 template <int N>
 struct Bars {
-  uint64_t b_full[Cfg<N>::kStagesB], b_empty[Cfg<N>::kStagesB];
-  uint64_t a_full[kStagesA], a_empty[kStagesA];
+  uint64_t full[Cfg<N>::kStages], empty[Cfg<N>::kStages];
   uint64_t raw_full[kStagesRaw], raw_empty[kStagesRaw];
   uint64_t acc_full[2], acc_empty[2];
   uint64_t drained;
   uint32_t tmem_base;
-  int abort;
 };
 
 // MN-major, 128-byte swizzle: 64 elements x 8 tokens are 1024 bytes; the next 8 tokens follow at once,
@@ -116,6 +113,12 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, i
       : "memory");
 }
 
+__device__ __forceinline__ bool elect_one() {
+  uint32_t leader;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(leader));
+  return leader != 0;
+}
+
 // A unit of work: one tile and one share of the tokens.  Units of one share are neighbours, so the
 // blocks that run at the same time read the same tokens.
 struct Unit {
@@ -151,22 +154,19 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
                                                                   const __grid_constant__ CUtensorMap map_codes, Params prm) {
   using C = Cfg<N>;
   extern __shared__ unsigned char smem_raw[];
-  unsigned char* stages_b =
+  unsigned char* stages =
       reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  unsigned char* stages_a = stages_b + (size_t)C::kStagesB * C::kStageB;
-  unsigned char* raws = stages_a + (size_t)kStagesA * kStageA;
+  unsigned char* raws = stages + (size_t)C::kStages * C::kStage;
   Bars<N>* bars = reinterpret_cast<Bars<N>*>(raws + (size_t)kStagesRaw * kRawBytes);
   static_assert(sizeof(Bars<N>) <= 256, "barrier block");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int units = prm.tiles * prm.splits;
 
   if (tid == 0) {
-    for (int s = 0; s < C::kStagesB; ++s) { mbar_init(&bars->b_full[s], 1); mbar_init(&bars->b_empty[s], 1); }
-    for (int s = 0; s < kStagesA; ++s) { mbar_init(&bars->a_full[s], 4); mbar_init(&bars->a_empty[s], 1); }
+    for (int s = 0; s < C::kStages; ++s) { mbar_init(&bars->full[s], 1 + 4); mbar_init(&bars->empty[s], 1); }
     for (int s = 0; s < kStagesRaw; ++s) { mbar_init(&bars->raw_full[s], 1 + 32); mbar_init(&bars->raw_empty[s], 4); }
     for (int s = 0; s < 2; ++s) { mbar_init(&bars->acc_full[s], 1); mbar_init(&bars->acc_empty[s], 4); }
     mbar_init(&bars->drained, 1);
-    bars->abort = 0;
     fence_proxy_async();
   }
   if (warp == 1) {
@@ -179,89 +179,76 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t*>(&bars->tmem_base);
-  volatile int* abort = &bars->abort;
-
+  // Every wait is bounded.  A role whose wait ran out leaves its loop, the others' waits then run out as
+  // well, and the read-out writes NaN.  (A shared flag looked at after every wait cost 8 % of the run time.)
   if (warp == 0) {
     // ---------------- codes and dY by TMA
-    if (lane == 0) {
-      uint32_t n = 0, nr = 0;                           // stages of dY and of codes asked for so far
+    if (elect_one()) {
+      uint32_t n = 0;                                   // steps asked for so far
       bool ok = true;
       for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
         const Unit w = unit_of(prm, u, N);
-        for (int k = w.k0; k < w.k1 && ok; ++k) {
-          const int r = nr % kStagesRaw;
-          if (!mbar_wait(&bars->raw_empty[r], ((nr / kStagesRaw) & 1) ^ 1) || *abort) { ok = false; break; }
+        int k = w.k0 / prm.planes, pl = w.k0 - k * prm.planes;
+        for (int j = w.k0; j < w.k1; ++j, ++n) {
+          const int r = n % kStagesRaw, s = n % C::kStages;
+          ok = mbar_wait(&bars->raw_empty[r], ((n / kStagesRaw) & 1) ^ 1);
+          if (!ok) break;
           mbar_arrive_expect_tx(&bars->raw_full[r], kCodeBytes);
           tma_load_2d(raws + (size_t)r * kRawBytes, &map_codes, w.i0, k * kTokens, &bars->raw_full[r]);
-          ++nr;
-          for (int pl = 0; pl < prm.planes; ++pl) {
-            const int s = n % C::kStagesB;
-            if (!mbar_wait(&bars->b_empty[s], ((n / C::kStagesB) & 1) ^ 1) || *abort) { ok = false; break; }
-            mbar_arrive_expect_tx(&bars->b_full[s], C::kStageB);
+          ok = mbar_wait(&bars->empty[s], ((n / C::kStages) & 1) ^ 1);
+          if (!ok) break;
+          mbar_arrive_expect_tx(&bars->full[s], C::kBytesB);
+          unsigned char* b = stages + (size_t)s * C::kStage + kBytesA;
 #pragma unroll
-            for (int q = 0; q < N / 64; ++q)
-              tma_load_3d(stages_b + (size_t)s * C::kStageB + q * kBoxBytes, &map_dy, w.o0 + q * 64, k * kTokens, pl,
-                          &bars->b_full[s]);
-            ++n;
-          }
+          for (int q = 0; q < N / 64; ++q)
+            tma_load_3d(b + q * kBoxBytes, &map_dy, w.o0 + q * 64, k * kTokens, pl, &bars->full[s]);
+          if (++pl == prm.planes) { pl = 0; ++k; }
         }
       }
-      if (!ok) *abort = 1;
       // copies still in flight must land before the block may exit
-      for (uint32_t m = n > (uint32_t)C::kStagesB ? n - C::kStagesB : 0; m < n; ++m)
-        (void)mbar_wait(&bars->b_full[m % C::kStagesB], (m / C::kStagesB) & 1);
-      for (uint32_t m = nr > (uint32_t)kStagesRaw ? nr - kStagesRaw : 0; m < nr; ++m)
-        (void)mbar_wait(&bars->raw_full[m % kStagesRaw], (m / kStagesRaw) & 1);
+      for (uint32_t m = n > (uint32_t)C::kStages ? n - C::kStages : 0; m < n; ++m)
+        (void)mbar_wait(&bars->full[m % C::kStages], (m / C::kStages) & 1);
+      if (!ok) (void)mbar_wait(&bars->raw_full[n % kStagesRaw], (n / kStagesRaw) & 1);
     }
+    __syncwarp();
   } else if (warp == 1) {
-    // ---------------- MMA: the warp waits together, one elected thread issues.  (With the whole role in an
-    // `if (lane == 0)` the products alone took a fifth longer: 579 against 484 us for 16384 x 4096 x 4096.)
-    uint32_t leader;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(leader));
-    uint32_t na = 0, nb = 0, nu = 0;
-    bool ok = true;
-    for (int u = blockIdx.x; u < units && ok; u += gridDim.x, ++nu) {
-      const Unit w = unit_of(prm, u, N);
-      const uint32_t acc = nu & 1, d = tmem_base + acc * N;
-      ok = __all_sync(0xffffffffu, mbar_wait(&bars->acc_empty[acc], ((nu >> 1) & 1) ^ 1) && !*abort);
-      for (int k = w.k0; k < w.k1 && ok; ++k, ++na) {
-        const int sa = na % kStagesA;
-        ok = __all_sync(0xffffffffu, mbar_wait(&bars->a_full[sa], (na / kStagesA) & 1) && !*abort);
-        const uint32_t a = smem_u32(stages_a + (size_t)sa * kStageA);
-        for (int pl = 0; pl < prm.planes && ok; ++pl, ++nb) {
-          const int sb = nb % C::kStagesB;
-          ok = __all_sync(0xffffffffu, mbar_wait(&bars->b_full[sb], (nb / C::kStagesB) & 1) && !*abort);
+    // ---------------- MMA: one elected thread.  (Chosen by `lane == 0` instead, the products alone took a fifth
+    // longer: 579 against 484 us for 16384 x 4096 x 4096.)
+    if (elect_one()) {
+      uint32_t n = 0, nu = 0;
+      bool ok = true;
+      for (int u = blockIdx.x; u < units && ok; u += gridDim.x, ++nu) {
+        const Unit w = unit_of(prm, u, N);
+        const uint32_t acc = nu & 1, d = tmem_base + acc * N;
+        ok = mbar_wait(&bars->acc_empty[acc], ((nu >> 1) & 1) ^ 1);
+        for (int j = w.k0; j < w.k1 && ok; ++j, ++n) {
+          const int s = n % C::kStages;
+          ok = mbar_wait(&bars->full[s], (n / C::kStages) & 1);
           if (!ok) break;
           tc_fence_after();
-          const uint32_t b = smem_u32(stages_b + (size_t)sb * C::kStageB);
-          if (leader) {
+          const uint32_t a = smem_u32(stages + (size_t)s * C::kStage), b = a + kBytesA;
 #pragma unroll
-            for (int q = 0; q < kTokens / 16; ++q)      // 16 tokens are two groups of 8: 2048 bytes
-              umma(d, mn_desc(a + q * 2048), mn_desc(b + q * 2048), C::kIdesc, (k == w.k0 && pl == 0 && q == 0) ? 0u : 1u);
-            umma_commit(&bars->b_empty[sb]);
-            if (pl == prm.planes - 1) umma_commit(&bars->a_empty[sa]);
-          }
-          __syncwarp();
+          for (int q = 0; q < kTokens / 16; ++q)        // 16 tokens are two groups of 8: 2048 bytes
+            umma(d, mn_desc(a + q * 2048), mn_desc(b + q * 2048), C::kIdesc, (j == w.k0 && q == 0) ? 0u : 1u);
+          umma_commit(&bars->empty[s]);
         }
+        if (ok) umma_commit(&bars->acc_full[acc]);
       }
-      if (ok && leader) umma_commit(&bars->acc_full[acc]);
-    }
-    if (!ok && leader) {                                // products under way must end before the block may exit
-      *abort = 1;
-      umma_commit(&bars->drained);
-      (void)mbar_wait(&bars->drained, 0);
+      if (!ok) {                                        // products under way must end before the block may exit
+        umma_commit(&bars->drained);
+        (void)mbar_wait(&bars->drained, 0);
+      }
     }
     __syncwarp();
   } else if (warp < 6) {
     // ---------------- read-out: warp w reads the 32 accumulator rows of its quarter
     const int quarter = warp & 3;
     uint32_t nu = 0;
+    bool ok = true;
     for (int u = blockIdx.x; u < units; u += gridDim.x, ++nu) {
       const Unit w = unit_of(prm, u, N);
       const uint32_t acc = nu & 1;
-      bool ok = !*abort && mbar_wait(&bars->acc_full[acc], (nu >> 1) & 1) && !*abort;
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok && lane == 0) *abort = 1;
+      ok = __all_sync(0xffffffffu, ok && mbar_wait(&bars->acc_full[acc], (nu >> 1) & 1));
       tc_fence_after();
       const int i = w.i0 + quarter * 32 + lane;
       float* part = prm.partials + (size_t)w.split * prm.split_stride;
@@ -299,56 +286,55 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
       const Unit w = unit_of(prm, u, N);
       total += w.k1 - w.k0;
     }
-    bool ok = true;
     for (int n = (warp - 6) >> 2; n < total; n += kConvGroups) {
-      const int s = n % kStagesA, r = n % kStagesRaw;
-      ok = __all_sync(0xffffffffu, mbar_wait(&bars->raw_full[r], (n / kStagesRaw) & 1) && !*abort);
-      if (!ok) break;
+      const int s = n % C::kStages, r = n % kStagesRaw;
+      if (!__all_sync(0xffffffffu, mbar_wait(&bars->raw_full[r], (n / kStagesRaw) & 1))) break;
       const unsigned char* raw = raws + (size_t)r * kRawBytes;
-      uint4 q[4];
+      uint4 q[4], lo[4], hi[4];
       uint32_t e[4];
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
         q[h] = *reinterpret_cast<const uint4*>(raw + (t + h * 16) * kIns + c * 16);
         e[h] = raw[kCodeBytes + (t + h * 16) * 4 + (c >> 1)];
       }
-      ok = __all_sync(0xffffffffu, mbar_wait(&bars->a_empty[s], ((n / kStagesA) & 1) ^ 1) && !*abort);
-      if (!ok) break;
-      unsigned char* base = stages_a + (size_t)s * kStageA + (c >> 2) * kBoxBytes;
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
         const __nv_bfloat162 sc = scale_bf16(e[h]);
         const uint4 x = q[h];
-        uint4 lo, hi;
-        lo.x = codes_to_bf16(__byte_perm(x.x, 0, 0x4140), sc); lo.y = codes_to_bf16(__byte_perm(x.x, 0, 0x4342), sc);
-        lo.z = codes_to_bf16(__byte_perm(x.y, 0, 0x4140), sc); lo.w = codes_to_bf16(__byte_perm(x.y, 0, 0x4342), sc);
-        hi.x = codes_to_bf16(__byte_perm(x.z, 0, 0x4140), sc); hi.y = codes_to_bf16(__byte_perm(x.z, 0, 0x4342), sc);
-        hi.z = codes_to_bf16(__byte_perm(x.w, 0, 0x4140), sc); hi.w = codes_to_bf16(__byte_perm(x.w, 0, 0x4342), sc);
+        lo[h].x = codes_to_bf16(__byte_perm(x.x, 0, 0x4140), sc); lo[h].y = codes_to_bf16(__byte_perm(x.x, 0, 0x4342), sc);
+        lo[h].z = codes_to_bf16(__byte_perm(x.y, 0, 0x4140), sc); lo[h].w = codes_to_bf16(__byte_perm(x.y, 0, 0x4342), sc);
+        hi[h].x = codes_to_bf16(__byte_perm(x.z, 0, 0x4140), sc); hi[h].y = codes_to_bf16(__byte_perm(x.z, 0, 0x4342), sc);
+        hi[h].z = codes_to_bf16(__byte_perm(x.w, 0, 0x4140), sc); hi[h].w = codes_to_bf16(__byte_perm(x.w, 0, 0x4342), sc);
+      }
+      if (!__all_sync(0xffffffffu, mbar_wait(&bars->empty[s], ((n / C::kStages) & 1) ^ 1))) break;
+      unsigned char* base = stages + (size_t)s * C::kStage + (c >> 2) * kBoxBytes;
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
         const int tt = t + h * 16;
         unsigned char* row = base + tt * 128;
         const int ch = (c & 3) * 2, swap = c >> 2;       // the upper half stores its odd chunk first: no two lanes on a bank
-        *reinterpret_cast<uint4*>(row + (((ch + swap) ^ (tt & 7)) << 4)) = swap ? hi : lo;
-        *reinterpret_cast<uint4*>(row + (((ch + 1 - swap) ^ (tt & 7)) << 4)) = swap ? lo : hi;
+        *reinterpret_cast<uint4*>(row + (((ch + swap) ^ (tt & 7)) << 4)) = swap ? hi[h] : lo[h];
+        *reinterpret_cast<uint4*>(row + (((ch + 1 - swap) ^ (tt & 7)) << 4)) = swap ? lo[h] : hi[h];
       }
       fence_proxy_async();
       __syncwarp();
       if (lane == 0) {
+        mbar_arrive(&bars->full[s]);
         mbar_arrive(&bars->raw_empty[r]);
-        mbar_arrive(&bars->a_full[s]);
       }
     }
-    if (!ok && lane == 0) *abort = 1;
   } else {
     // ---------------- scales: a lane copies the words of two tokens; words past the last token are zero
     // (their codes are zero as well), the copies' arrival is counted on the stage's barrier
-    uint32_t nr = 0;
+    uint32_t n = 0;
     bool ok = true;
     for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
       const Unit w = unit_of(prm, u, N);
       const uint8_t* column = prm.scales + (w.i0 >> 5);
-      for (int k = w.k0; k < w.k1; ++k, ++nr) {
-        const int r = nr % kStagesRaw;
-        ok = __all_sync(0xffffffffu, mbar_wait(&bars->raw_empty[r], ((nr / kStagesRaw) & 1) ^ 1) && !*abort);
+      int k = w.k0 / prm.planes, pl = w.k0 - k * prm.planes;
+      for (int j = w.k0; j < w.k1; ++j, ++n) {
+        const int r = n % kStagesRaw;
+        ok = __all_sync(0xffffffffu, mbar_wait(&bars->raw_empty[r], ((n / kStagesRaw) & 1) ^ 1));
         if (!ok) break;
         const uint32_t dst = smem_u32(raws + (size_t)r * kRawBytes + kCodeBytes);
 #pragma unroll
@@ -361,10 +347,10 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
                        : "memory");
         }
         asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&bars->raw_full[r])) : "memory");
+        if (++pl == prm.planes) { pl = 0; ++k; }
       }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");     // nothing of this thread's is in flight at exit
-    if (!ok && lane == 0) *abort = 1;
   }
 
   tc_fence_before();
@@ -432,7 +418,7 @@ Plan plan_of(long long rows, long long outs, long long ins, int dtype, bool pack
   p.n = outs <= 128 ? 128 : 256;
   p.tiles_i = static_cast<int>((ins + kIns - 1) / kIns);
   p.tiles_o = static_cast<int>((outs + p.n - 1) / p.n);
-  p.ksteps = static_cast<int>((rows + kTokens - 1) / kTokens);
+  p.ksteps = static_cast<int>((rows + kTokens - 1) / kTokens) * p.planes;
   const long long tiles = (long long)p.tiles_i * p.tiles_o;
   p.tiles = static_cast<int>(tiles);
   const int sms = sm_count();
