@@ -33,8 +33,14 @@ constexpr int kBoxBytes = 64 * kTokens * 2;          // 64 columns x 64 tokens o
 constexpr int kBytesA = 2 * kBoxBytes;
 constexpr int kCodeBytes = kIns * kTokens;           // codes of a stage as they are stored
 constexpr int kRawBytes = kCodeBytes + 4 * kTokens;  // and the scales of the tile's four groups, a word per token
-constexpr int kStagesRaw = 4;
-constexpr int kConvGroups = 3;                       // a group of four warps converts every third stage
+constexpr int kConvGroups = 3;                       // a group of four warps converts every third step
+// A stage of codes belongs to one group.  A wait tells two neighbouring phases of a barrier apart and no
+// more, so a role must not be able to arrive at a barrier two phases early:
+//   * codes: the group has itself used the stage's previous phase up;
+//   * `empty` of step n: the codes of step n are there, so those of step n - kStagesRaw were converted, which
+//     was after products n - kStagesRaw - kStages had ended, and with kStagesRaw <= kStages that is at most
+//     one phase before the one waited for.
+constexpr int kStagesRaw = kConvGroups;
 constexpr int kScaleWarp = 6 + 4 * kConvGroups;
 constexpr int kThreads = 32 * (kScaleWarp + 1);      // warp 0 TMA, 1 MMA, 2-5 read-out, 6.. converters, last scales
 
@@ -42,6 +48,7 @@ template <int N> struct Cfg {
   static constexpr int kBytesB = N / 64 * kBoxBytes;
   static constexpr int kStage = kBytesA + kBytesB;   // a stage: codes as bf16, then dY
   static constexpr int kStages = N == 256 ? 4 : 5;
+  static_assert(kStagesRaw <= kStages, "see kStagesRaw");
   static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + (size_t)kStagesRaw * kRawBytes + 256;
   // kind::f16: D fp32, A and B bf16, both MN-major, M = 128
   static constexpr uint32_t kIdesc =
