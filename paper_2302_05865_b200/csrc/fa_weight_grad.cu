@@ -37,9 +37,8 @@ constexpr int kConvGroups = 3;                       // a group of four warps co
 // A stage of codes belongs to one group.  A wait tells two neighbouring phases of a barrier apart and no
 // more, so a role must not be able to arrive at a barrier two phases early:
 //   * codes: the group has itself used the stage's previous phase up;
-//   * `empty` of step n: the codes of step n are there, so those of step n - kStagesRaw were converted, which
-//     was after products n - kStagesRaw - kStages had ended, and with kStagesRaw <= kStages that is at most
-//     one phase before the one waited for.
+//   * `empty` of step n: the group has done step n - kConvGroups, for which products n - kConvGroups - kStages
+//     had ended; with kConvGroups <= kStages that is at most one phase before the one waited for.
 constexpr int kStagesRaw = kConvGroups;
 constexpr int kScaleWarp = 6 + 4 * kConvGroups;
 constexpr int kThreads = 32 * (kScaleWarp + 1);      // warp 0 TMA, 1 MMA, 2-5 read-out, 6.. converters, last scales
@@ -48,7 +47,7 @@ template <int N> struct Cfg {
   static constexpr int kBytesB = N / 64 * kBoxBytes;
   static constexpr int kStage = kBytesA + kBytesB;   // a stage: codes as bf16, then dY
   static constexpr int kStages = N == 256 ? 4 : 5;
-  static_assert(kStagesRaw <= kStages, "see kStagesRaw");
+  static_assert(kConvGroups <= kStages && kStagesRaw % kConvGroups == 0, "see kStagesRaw");
   static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + (size_t)kStagesRaw * kRawBytes + 256;
   // kind::f16: D fp32, A and B bf16, both MN-major, M = 128
   static constexpr uint32_t kIdesc =
@@ -150,9 +149,11 @@ __device__ __forceinline__ uint32_t codes_to_bf16(uint32_t x, __nv_bfloat162 sca
   __nv_bfloat162 v = __hmul2(__hsub2(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b)), scale);
   return *reinterpret_cast<uint32_t*>(&v);
 }
+// The scale, twice.  The byte is a bf16's exponent, except that 2^-127 has the bits 0x0040; 255 gives Inf, and
+// the codes of such a group are 0, so that the products are NaN.
 __device__ __forceinline__ __nv_bfloat162 scale_bf16(uint32_t byte) {
-  uint32_t s = byte == 255u ? 0x7FC0u : byte == 0u ? 0x0040u : byte << 7;
-  s |= s << 16;
+  uint32_t s = byte * 0x00800080u;
+  if (byte == 0) s = 0x00400040u;
   return *reinterpret_cast<__nv_bfloat162*>(&s);
 }
 
@@ -286,8 +287,11 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
       if (lane == 0) mbar_arrive(&bars->acc_empty[acc]);
     }
   } else if (warp < kScaleWarp) {
-    // ---------------- converters: thread -> 16 codes of tokens t, t + 16, t + 32, t + 48 of the stage
-    const int ct = (tid - 192) & 127, c = ct & 7, t = ct >> 3;
+    // ---------------- converters: thread -> 8 codes of tokens t, t + 8, ..., t + 56 of the stage.  All eight
+    // lie at fixed distances, in the codes as in the swizzled operand (the swizzle goes by t mod 8).
+    const int ct = (tid - 192) & 127, c = ct & 15, t = ct >> 4;
+    const uint32_t from = t * kIns + c * 8, scale_from = kCodeBytes + t * 4 + (c >> 2);
+    const uint32_t to = (c >> 3) * kBoxBytes + t * 128 + (((c & 7) ^ t) << 4);
     int total = 0;
     for (int u = blockIdx.x; u < units; u += gridDim.x) {
       const Unit w = unit_of(prm, u, N);
@@ -297,38 +301,31 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
       const int s = n % C::kStages, r = n % kStagesRaw;
       if (!__all_sync(0xffffffffu, mbar_wait(&bars->raw_full[r], (n / kStagesRaw) & 1))) break;
       const unsigned char* raw = raws + (size_t)r * kRawBytes;
-      uint4 q[4], lo[4], hi[4];
-      uint32_t e[4];
+      uint2 q[8];
+      uint32_t e[8];
+      uint4 v[8];
 #pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        q[h] = *reinterpret_cast<const uint4*>(raw + (t + h * 16) * kIns + c * 16);
-        e[h] = raw[kCodeBytes + (t + h * 16) * 4 + (c >> 1)];
+      for (int h = 0; h < 8; ++h) {
+        q[h] = *reinterpret_cast<const uint2*>(raw + from + h * 8 * kIns);
+        e[h] = raw[scale_from + h * 32];
       }
 #pragma unroll
-      for (int h = 0; h < 4; ++h) {
+      for (int h = 0; h < 8; ++h) {
         const __nv_bfloat162 sc = scale_bf16(e[h]);
-        const uint4 x = q[h];
-        lo[h].x = codes_to_bf16(__byte_perm(x.x, 0, 0x4140), sc); lo[h].y = codes_to_bf16(__byte_perm(x.x, 0, 0x4342), sc);
-        lo[h].z = codes_to_bf16(__byte_perm(x.y, 0, 0x4140), sc); lo[h].w = codes_to_bf16(__byte_perm(x.y, 0, 0x4342), sc);
-        hi[h].x = codes_to_bf16(__byte_perm(x.z, 0, 0x4140), sc); hi[h].y = codes_to_bf16(__byte_perm(x.z, 0, 0x4342), sc);
-        hi[h].z = codes_to_bf16(__byte_perm(x.w, 0, 0x4140), sc); hi[h].w = codes_to_bf16(__byte_perm(x.w, 0, 0x4342), sc);
+        v[h].x = codes_to_bf16(__byte_perm(q[h].x, 0, 0x4140), sc);
+        v[h].y = codes_to_bf16(__byte_perm(q[h].x, 0, 0x4342), sc);
+        v[h].z = codes_to_bf16(__byte_perm(q[h].y, 0, 0x4140), sc);
+        v[h].w = codes_to_bf16(__byte_perm(q[h].y, 0, 0x4342), sc);
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars->raw_empty[r]);     // every lane has its codes
       if (!__all_sync(0xffffffffu, mbar_wait(&bars->empty[s], ((n / C::kStages) & 1) ^ 1))) break;
-      unsigned char* base = stages + (size_t)s * C::kStage + (c >> 2) * kBoxBytes;
+      unsigned char* dst = stages + (size_t)s * C::kStage + to;
 #pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        const int tt = t + h * 16;
-        unsigned char* row = base + tt * 128;
-        const int ch = (c & 3) * 2, swap = c >> 2;       // the upper half stores its odd chunk first: no two lanes on a bank
-        *reinterpret_cast<uint4*>(row + (((ch + swap) ^ (tt & 7)) << 4)) = swap ? hi[h] : lo[h];
-        *reinterpret_cast<uint4*>(row + (((ch + 1 - swap) ^ (tt & 7)) << 4)) = swap ? lo[h] : hi[h];
-      }
+      for (int h = 0; h < 8; ++h) *reinterpret_cast<uint4*>(dst + h * 1024) = v[h];
       fence_proxy_async();
       __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(&bars->full[s]);
-        mbar_arrive(&bars->raw_empty[r]);
-      }
+      if (lane == 0) mbar_arrive(&bars->full[s]);
     }
   } else {
     // ---------------- scales: a lane copies the words of two tokens; words past the last token are zero
