@@ -34,24 +34,29 @@ constexpr int kBytesA = 2 * kBoxBytes;
 constexpr int kCodeBytes = kIns * kTokens;           // codes of a stage as they are stored
 constexpr int kRawBytes = kCodeBytes + 4 * kTokens;  // and the scales of the tile's four groups, a word per token
 constexpr int kConvGroups = 3;                       // a group of four warps converts every third step
-// A stage of codes belongs to one group.  A wait tells two neighbouring phases of a barrier apart and no
-// more, so a role must not be able to arrive at a barrier two phases early:
-//   * codes: the group has itself used the stage's previous phase up;
+// A wait tells two neighbouring phases of a barrier apart and no more, so a role must not be able to arrive at a
+// barrier two phases early.  For the converter groups, which skip steps:
+//   * a stage of codes belongs to one group (kStagesRaw is a multiple of kConvGroups), which has itself used the
+//     stage's previous phase up;
 //   * `empty` of step n: the group has done step n - kConvGroups, for which products n - kConvGroups - kStages
 //     had ended; with kConvGroups <= kStages that is at most one phase before the one waited for.
-constexpr int kStagesRaw = kConvGroups;
 constexpr int kScaleWarp = 6 + 4 * kConvGroups;
 constexpr int kThreads = 32 * (kScaleWarp + 1);      // warp 0 TMA, 1 MMA, 2-5 read-out, 6.. converters, last scales
 
-template <int N> struct Cfg {
-  static constexpr int kBytesB = N / 64 * kBoxBytes;
+// A tile of kIns * PAIR inputs x N outputs, by one block or by a pair of blocks on neighbouring SMs.  In a pair each
+// block holds its own 128 inputs and half of dY's columns, and the tensor cores read the other half from the
+// neighbour.  Shared memory moves 128 bytes a cycle for the copies, the converters and the products together: for
+// N = 256 a step costs 898 of its cycles with one block and 642 with a pair, and the products take 512.
+template <int N, int PAIR> struct Cfg {
+  static constexpr int kBytesB = N / PAIR / 64 * kBoxBytes;
   static constexpr int kStage = kBytesA + kBytesB;   // a stage: codes as bf16, then dY
-  static constexpr int kStages = N == 256 ? 4 : 5;
-  static_assert(kConvGroups <= kStages && kStagesRaw % kConvGroups == 0, "see kStagesRaw");
+  static constexpr int kStages = N / PAIR == 256 ? 4 : 5;
+  static constexpr int kStagesRaw = N / PAIR == 256 ? kConvGroups : 2 * kConvGroups;
+  static_assert(kConvGroups <= kStages && kStagesRaw % kConvGroups == 0, "see the note on phases");
   static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + (size_t)kStagesRaw * kRawBytes + 256;
-  // kind::f16: D fp32, A and B bf16, both MN-major, M = 128
-  static constexpr uint32_t kIdesc =
-      (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(N >> 3) << 17) | ((128u >> 4) << 24);
+  // kind::f16: D fp32, A and B bf16, both MN-major, M = 128 or 256
+  static constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) |
+                                     ((uint32_t)(N >> 3) << 17) | ((uint32_t)(kIns * PAIR >> 4) << 24);
 };
 
 struct Params {
@@ -69,11 +74,11 @@ struct Params {
   size_t split_stride;
 };
 
-template <int N>
+template <int N, int PAIR>
 struct Bars {
-  uint64_t full[Cfg<N>::kStages], empty[Cfg<N>::kStages];
-  uint64_t raw_full[kStagesRaw], raw_empty[kStagesRaw];
-  uint64_t acc_full[2], acc_empty[2];
+  uint64_t full[Cfg<N, PAIR>::kStages], empty[Cfg<N, PAIR>::kStages];      // full: of the pair's first block
+  uint64_t raw_full[Cfg<N, PAIR>::kStagesRaw], raw_empty[Cfg<N, PAIR>::kStagesRaw];
+  uint64_t acc_full[2], acc_empty[2];                                      // acc_empty: of the pair's first block
   uint64_t drained;
   uint32_t tmem_base;
 };
@@ -85,16 +90,56 @@ __device__ __forceinline__ uint64_t mn_desc(uint32_t saddr) {
          ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
 
+template <int PAIR>
 __device__ __forceinline__ void umma(uint32_t tmem_d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d),
-      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-      : "memory");
+  if constexpr (PAIR == 1)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
 }
+// The barrier (in a pair: both blocks') is arrived at when the products issued so far have ended.
+template <int PAIR>
 __device__ __forceinline__ void umma_commit(uint64_t* bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
-               : "memory");
+  if constexpr (PAIR == 1)
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
+                 : "memory");
+  else
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+            smem_u32(bar)),
+        "h"((uint16_t)3)
+        : "memory");
+}
+// Address of the same place in the pair's first block.
+__device__ __forceinline__ uint32_t in_first(uint32_t saddr) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(saddr));
+  return a;
+}
+// Hands something of this SM (an operand that fence.proxy.async has shown to its tensor core, or accumulators
+// read out) over to the thread that issues the products.  No data of this SM is read by that thread, so the
+// arrival needs no order of other SMs' memory: as a release for the whole cluster it took half as long again
+// as the step it hands over (711 against 484 us for 16384 x 4096 x 4096).
+template <int PAIR>
+__device__ __forceinline__ void arrive_first(uint64_t* bar) {
+  if constexpr (PAIR == 1) mbar_arrive(bar);
+  else asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(in_first(smem_u32(bar))) : "memory");
+}
+template <int PAIR>
+__device__ __forceinline__ void sync_all() {
+  if constexpr (PAIR == 1) {
+    __syncthreads();
+  } else {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
 }
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&v)[32]) {
   asm volatile(
@@ -111,12 +156,21 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&v)[32]) {
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
+// A box of dY into this block's memory; its bytes are counted on the barrier of the pair's first block.
+template <int PAIR>
 __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
-          smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
-      : "memory");
+  if constexpr (PAIR == 1)
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+            smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+        : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, "
+        "%4}], [%5];" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(in_first(smem_u32(bar)))
+        : "memory");
 }
 
 __device__ __forceinline__ bool elect_one() {
@@ -125,18 +179,19 @@ __device__ __forceinline__ bool elect_one() {
   return leader != 0;
 }
 
-// A unit of work: one tile and one share of the tokens.  Units of one share are neighbours, so the
+// A unit of work of a block or pair: one tile and one share of the tokens.  Units of one share are neighbours, so the
 // blocks that run at the same time read the same tokens.
 struct Unit {
   int i0, o0, split, k0, k1;
 };
-__device__ __forceinline__ Unit unit_of(const Params& p, int u, int n) {
+template <int N, int PAIR>
+__device__ __forceinline__ Unit unit_of(const Params& p, int u, int rank) {
   Unit w;
   w.split = u / p.tiles;
   const int tile = u - w.split * p.tiles;
   const int oi = tile / p.tiles_i;
-  w.i0 = (tile - oi * p.tiles_i) * kIns;
-  w.o0 = oi * n;
+  w.i0 = ((tile - oi * p.tiles_i) * PAIR + rank) * kIns;
+  w.o0 = oi * N;
   w.k0 = (int)((long long)p.ksteps * w.split / p.splits);
   w.k1 = (int)((long long)p.ksteps * (w.split + 1) / p.splits);
   return w;
@@ -157,34 +212,44 @@ __device__ __forceinline__ __nv_bfloat162 scale_bf16(uint32_t byte) {
   return *reinterpret_cast<__nv_bfloat162*>(&s);
 }
 
-template <int N>
+template <int N, int PAIR>
 __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_constant__ CUtensorMap map_dy,
                                                                   const __grid_constant__ CUtensorMap map_codes, Params prm) {
-  using C = Cfg<N>;
+  using C = Cfg<N, PAIR>;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* stages =
       reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   unsigned char* raws = stages + (size_t)C::kStages * C::kStage;
-  Bars<N>* bars = reinterpret_cast<Bars<N>*>(raws + (size_t)kStagesRaw * kRawBytes);
-  static_assert(sizeof(Bars<N>) <= 256, "barrier block");
+  Bars<N, PAIR>* bars = reinterpret_cast<Bars<N, PAIR>*>(raws + (size_t)C::kStagesRaw * kRawBytes);
+  static_assert(sizeof(Bars<N, PAIR>) <= 256, "barrier block");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int units = prm.tiles * prm.splits;
+  const int rank = PAIR == 1 ? 0 : blockIdx.x & 1, first_unit = blockIdx.x / PAIR, unit_step = gridDim.x / PAIR;
 
   if (tid == 0) {
-    for (int s = 0; s < C::kStages; ++s) { mbar_init(&bars->full[s], 1 + 4); mbar_init(&bars->empty[s], 1); }
-    for (int s = 0; s < kStagesRaw; ++s) { mbar_init(&bars->raw_full[s], 1 + 32); mbar_init(&bars->raw_empty[s], 4); }
-    for (int s = 0; s < 2; ++s) { mbar_init(&bars->acc_full[s], 1); mbar_init(&bars->acc_empty[s], 4); }
+    for (int s = 0; s < C::kStages; ++s) { mbar_init(&bars->full[s], 1 + 4 * PAIR); mbar_init(&bars->empty[s], 1); }
+    for (int s = 0; s < C::kStagesRaw; ++s) { mbar_init(&bars->raw_full[s], 1 + 32); mbar_init(&bars->raw_empty[s], 4); }
+    for (int s = 0; s < 2; ++s) { mbar_init(&bars->acc_full[s], 1); mbar_init(&bars->acc_empty[s], 4 * PAIR); }
     mbar_init(&bars->drained, 1);
+    if (PAIR > 1) asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_proxy_async();
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)),
-                 "r"(2 * N)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if constexpr (PAIR == 1) {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)),
+                   "r"(2 * N)
+                   : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)),
+                   "r"(2 * N)
+                   : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
   }
   tc_fence_before();
   __syncthreads();
+  sync_all<PAIR>();
   tc_fence_after();
   const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t*>(&bars->tmem_base);
   // Every wait is bounded.  A role whose wait ran out leaves its loop, the others' waits then run out as
@@ -194,39 +259,39 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
     if (elect_one()) {
       uint32_t n = 0;                                   // steps asked for so far
       bool ok = true;
-      for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
-        const Unit w = unit_of(prm, u, N);
+      for (int u = first_unit; u < units && ok; u += unit_step) {
+        const Unit w = unit_of<N, PAIR>(prm, u, rank);
         int k = w.k0 / prm.planes, pl = w.k0 - k * prm.planes;
         for (int j = w.k0; j < w.k1; ++j, ++n) {
-          const int r = n % kStagesRaw, s = n % C::kStages;
-          ok = mbar_wait(&bars->raw_empty[r], ((n / kStagesRaw) & 1) ^ 1);
+          const int r = n % C::kStagesRaw, s = n % C::kStages;
+          ok = mbar_wait(&bars->raw_empty[r], ((n / C::kStagesRaw) & 1) ^ 1);
           if (!ok) break;
           mbar_arrive_expect_tx(&bars->raw_full[r], kCodeBytes);
           tma_load_2d(raws + (size_t)r * kRawBytes, &map_codes, w.i0, k * kTokens, &bars->raw_full[r]);
           ok = mbar_wait(&bars->empty[s], ((n / C::kStages) & 1) ^ 1);
           if (!ok) break;
-          mbar_arrive_expect_tx(&bars->full[s], C::kBytesB);
+          if (rank == 0) mbar_arrive_expect_tx(&bars->full[s], PAIR * C::kBytesB);
           unsigned char* b = stages + (size_t)s * C::kStage + kBytesA;
 #pragma unroll
-          for (int q = 0; q < N / 64; ++q)
-            tma_load_3d(b + q * kBoxBytes, &map_dy, w.o0 + q * 64, k * kTokens, pl, &bars->full[s]);
+          for (int q = 0; q < N / PAIR / 64; ++q)
+            tma_load_3d<PAIR>(b + q * kBoxBytes, &map_dy, w.o0 + rank * (N / PAIR) + q * 64, k * kTokens, pl, &bars->full[s]);
           if (++pl == prm.planes) { pl = 0; ++k; }
         }
       }
       // copies still in flight must land before the block may exit
       for (uint32_t m = n > (uint32_t)C::kStages ? n - C::kStages : 0; m < n; ++m)
-        (void)mbar_wait(&bars->full[m % C::kStages], (m / C::kStages) & 1);
-      if (!ok) (void)mbar_wait(&bars->raw_full[n % kStagesRaw], (n / kStagesRaw) & 1);
+        (void)mbar_wait(&bars->empty[m % C::kStages], (m / C::kStages) & 1);
+      if (!ok) (void)mbar_wait(&bars->raw_full[n % C::kStagesRaw], (n / C::kStagesRaw) & 1);
     }
     __syncwarp();
   } else if (warp == 1) {
     // ---------------- MMA: one elected thread.  (Chosen by `lane == 0` instead, the products alone took a fifth
     // longer: 579 against 484 us for 16384 x 4096 x 4096.)
-    if (elect_one()) {
+    if (rank == 0 && elect_one()) {
       uint32_t n = 0, nu = 0;
       bool ok = true;
-      for (int u = blockIdx.x; u < units && ok; u += gridDim.x, ++nu) {
-        const Unit w = unit_of(prm, u, N);
+      for (int u = first_unit; u < units && ok; u += unit_step, ++nu) {
+        const Unit w = unit_of<N, PAIR>(prm, u, rank);
         const uint32_t acc = nu & 1, d = tmem_base + acc * N;
         ok = mbar_wait(&bars->acc_empty[acc], ((nu >> 1) & 1) ^ 1);
         for (int j = w.k0; j < w.k1 && ok; ++j, ++n) {
@@ -237,13 +302,13 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
           const uint32_t a = smem_u32(stages + (size_t)s * C::kStage), b = a + kBytesA;
 #pragma unroll
           for (int q = 0; q < kTokens / 16; ++q)        // 16 tokens are two groups of 8: 2048 bytes
-            umma(d, mn_desc(a + q * 2048), mn_desc(b + q * 2048), C::kIdesc, (j == w.k0 && q == 0) ? 0u : 1u);
-          umma_commit(&bars->empty[s]);
+            umma<PAIR>(d, mn_desc(a + q * 2048), mn_desc(b + q * 2048), C::kIdesc, (j == w.k0 && q == 0) ? 0u : 1u);
+          umma_commit<PAIR>(&bars->empty[s]);
         }
-        if (ok) umma_commit(&bars->acc_full[acc]);
+        if (ok) umma_commit<PAIR>(&bars->acc_full[acc]);
       }
       if (!ok) {                                        // products under way must end before the block may exit
-        umma_commit(&bars->drained);
+        umma_commit<PAIR>(&bars->drained);
         (void)mbar_wait(&bars->drained, 0);
       }
     }
@@ -253,8 +318,8 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
     const int quarter = warp & 3;
     uint32_t nu = 0;
     bool ok = true;
-    for (int u = blockIdx.x; u < units; u += gridDim.x, ++nu) {
-      const Unit w = unit_of(prm, u, N);
+    for (int u = first_unit; u < units; u += unit_step, ++nu) {
+      const Unit w = unit_of<N, PAIR>(prm, u, rank);
       const uint32_t acc = nu & 1;
       ok = __all_sync(0xffffffffu, ok && mbar_wait(&bars->acc_full[acc], (nu >> 1) & 1));
       tc_fence_after();
@@ -284,7 +349,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&bars->acc_empty[acc]);
+      if (lane == 0) arrive_first<PAIR>(&bars->acc_empty[acc]);
     }
   } else if (warp < kScaleWarp) {
     // ---------------- converters: thread -> 8 codes of tokens t, t + 8, ..., t + 56 of the stage.  All eight
@@ -293,13 +358,13 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
     const uint32_t from = t * kIns + c * 8, scale_from = kCodeBytes + t * 4 + (c >> 2);
     const uint32_t to = (c >> 3) * kBoxBytes + t * 128 + (((c & 7) ^ t) << 4);
     int total = 0;
-    for (int u = blockIdx.x; u < units; u += gridDim.x) {
-      const Unit w = unit_of(prm, u, N);
+    for (int u = first_unit; u < units; u += unit_step) {
+      const Unit w = unit_of<N, PAIR>(prm, u, rank);
       total += w.k1 - w.k0;
     }
     for (int n = (warp - 6) >> 2; n < total; n += kConvGroups) {
-      const int s = n % C::kStages, r = n % kStagesRaw;
-      if (!__all_sync(0xffffffffu, mbar_wait(&bars->raw_full[r], (n / kStagesRaw) & 1))) break;
+      const int s = n % C::kStages, r = n % C::kStagesRaw;
+      if (!__all_sync(0xffffffffu, mbar_wait(&bars->raw_full[r], (n / C::kStagesRaw) & 1))) break;
       const unsigned char* raw = raws + (size_t)r * kRawBytes;
       uint2 q[8];
       uint32_t e[8];
@@ -325,20 +390,21 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
       for (int h = 0; h < 8; ++h) *reinterpret_cast<uint4*>(dst + h * 1024) = v[h];
       fence_proxy_async();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&bars->full[s]);
+      if (lane == 0) arrive_first<PAIR>(&bars->full[s]);
     }
   } else {
     // ---------------- scales: a lane copies the words of two tokens; words past the last token are zero
     // (their codes are zero as well), the copies' arrival is counted on the stage's barrier
     uint32_t n = 0;
     bool ok = true;
-    for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
-      const Unit w = unit_of(prm, u, N);
-      const uint8_t* column = prm.scales + (w.i0 >> 5);
+    for (int u = first_unit; u < units && ok; u += unit_step) {
+      const Unit w = unit_of<N, PAIR>(prm, u, rank);
+      // (the second block of a pair may have no inputs at all: its results are not stored)
+      const uint8_t* column = prm.scales + ((w.i0 >> 5) < prm.scale_pitch ? w.i0 >> 5 : 0);
       int k = w.k0 / prm.planes, pl = w.k0 - k * prm.planes;
       for (int j = w.k0; j < w.k1; ++j, ++n) {
-        const int r = n % kStagesRaw;
-        ok = __all_sync(0xffffffffu, mbar_wait(&bars->raw_empty[r], ((n / kStagesRaw) & 1) ^ 1));
+        const int r = n % C::kStagesRaw;
+        ok = __all_sync(0xffffffffu, mbar_wait(&bars->raw_empty[r], ((n / C::kStagesRaw) & 1) ^ 1));
         if (!ok) break;
         const uint32_t dst = smem_u32(raws + (size_t)r * kRawBytes + kCodeBytes);
 #pragma unroll
@@ -359,9 +425,13 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
 
   tc_fence_before();
   __syncthreads();
+  sync_all<PAIR>();                          // neither block of a pair leaves while the other may still reach into it
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(2 * N) : "memory");
+    if constexpr (PAIR == 1)
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(2 * N) : "memory");
+    else
+      asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(2 * N) : "memory");
   }
 }
 
@@ -407,7 +477,7 @@ __global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ dy, lon
 // How a product is cut up.  Per block and stage the MMA takes N / 256 * 512 cycles or so; a split costs
 // a write and a read of the whole result.
 struct Plan {
-  int n, tiles_i, tiles_o, tiles, splits, ksteps, planes;
+  int n, pair, tiles_i, tiles_o, tiles, splits, ksteps, planes;
   bool pack;
   int pitch;
   size_t pack_bytes, split_stride;
@@ -420,12 +490,13 @@ Plan plan_of(long long rows, long long outs, long long ins, int dtype, bool pack
   p.pitch = static_cast<int>((outs + 7) / 8 * 8);
   p.pack_bytes = pack ? ((size_t)p.planes * rows * p.pitch * 2 + 255) / 256 * 256 : 0;
   p.n = outs <= 128 ? 128 : 256;
-  p.tiles_i = static_cast<int>((ins + kIns - 1) / kIns);
+  p.pair = ins > kIns && outs > 128 ? 2 : 1;
+  p.tiles_i = static_cast<int>((ins + kIns * p.pair - 1) / (kIns * p.pair));
   p.tiles_o = static_cast<int>((outs + p.n - 1) / p.n);
   p.ksteps = static_cast<int>((rows + kTokens - 1) / kTokens) * p.planes;
   const long long tiles = (long long)p.tiles_i * p.tiles_o;
   p.tiles = static_cast<int>(tiles);
-  const int sms = sm_count();
+  const int sms = sm_count() / p.pair;
   // splits that fill the blocks once; each keeps at least 4 stages
   long long s = tiles >= sms ? 1 : sms / tiles;
   if (s > (p.ksteps + 3) / 4) s = (p.ksteps + 3) / 4;
@@ -442,16 +513,26 @@ size_t linear_weight_grad_scratch_bytes(long long rows, long long outs, long lon
   return p.pack_bytes + (p.splits > 1 ? p.splits * p.split_stride * sizeof(float) : 0);
 }
 
-template <int N>
+template <int N, int PAIR>
 static cudaError_t launch_product(const CUtensorMap& map, const CUtensorMap& map_codes, const wgrad::Params& prm,
                                   cudaStream_t st) {
-  using C = wgrad::Cfg<N>;
-  cudaError_t e = cudaFuncSetAttribute(wgrad::weight_grad_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(C::kSmem));
+  using C = wgrad::Cfg<N, PAIR>;
+  auto kernel = wgrad::weight_grad_kernel<N, PAIR>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(C::kSmem));
   if (e != cudaSuccess) return e;
-  const int units = prm.tiles * prm.splits, sms = sm_count();
-  wgrad::weight_grad_kernel<N><<<units < sms ? units : sms, wgrad::kThreads, C::kSmem, st>>>(map, map_codes, prm);
-  return cudaGetLastError();
+  const int units = prm.tiles * prm.splits, most = sm_count() / PAIR;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(PAIR * (units < most ? units : most));
+  cfg.blockDim = dim3(wgrad::kThreads);
+  cfg.dynamicSmemBytes = C::kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute cluster{};
+  cluster.id = cudaLaunchAttributeClusterDimension;
+  cluster.val.clusterDim.x = PAIR;
+  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+  cfg.attrs = &cluster;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, map, map_codes, prm);
 }
 
 cudaError_t launch_linear_weight_grad(Mat dy, int dtype, long long rows, long long outs, long long ins, const void* ck,
@@ -506,7 +587,9 @@ cudaError_t launch_linear_weight_grad(Mat dy, int dtype, long long rows, long lo
   prm.dw = dweight; prm.gbf16 = gdtype == FA_BF16;
   prm.partials = reinterpret_cast<float*>(static_cast<char*>(scratch) + p.pack_bytes);
   prm.split_stride = p.split_stride;
-  cudaError_t e = p.n == 256 ? launch_product<256>(map, map_codes, prm, st) : launch_product<128>(map, map_codes, prm, st);
+  cudaError_t e = p.pair == 2  ? launch_product<256, 2>(map, map_codes, prm, st)
+                  : p.n == 256 ? launch_product<256, 1>(map, map_codes, prm, st)
+                               : launch_product<128, 1>(map, map_codes, prm, st);
   if (e != cudaSuccess || p.splits == 1) return e;
   wgrad::add_splits_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(prm.partials, p.split_stride, p.splits, n, dweight,
                                                                        prm.gbf16);
