@@ -41,7 +41,7 @@ constexpr int kConvGroups = 3;                       // a group of four warps co
 //   * `empty` of step n: the group has done step n - kConvGroups, for which products n - kConvGroups - kStages
 //     had ended; with kConvGroups <= kStages that is at most one phase before the one waited for.
 constexpr int kScaleWarp = 6 + 4 * kConvGroups;
-constexpr int kThreads = 32 * (kScaleWarp + 1);      // warp 0 TMA, 1 MMA, 2-5 read-out, 6.. converters, last scales
+constexpr int kThreads = 32 * (kScaleWarp + 1);      // warp 0 TMA, 1 MMA, 2-5 read-out, 6.. converters, last codes
 
 // A tile of kIns * PAIR inputs x N outputs, by one block or by a pair of blocks on neighbouring SMs.  In a pair each
 // block holds its own 128 inputs and half of dY's columns, and the tensor cores read the other half from the
@@ -255,7 +255,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
   // Every wait is bounded.  A role whose wait ran out leaves its loop, the others' waits then run out as
   // well, and the read-out writes NaN.  (A shared flag looked at after every wait cost 8 % of the run time.)
   if (warp == 0) {
-    // ---------------- codes and dY by TMA
+    // ---------------- dY by TMA
     if (elect_one()) {
       uint32_t n = 0;                                   // steps asked for so far
       bool ok = true;
@@ -263,11 +263,7 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
         const Unit w = unit_of<N, PAIR>(prm, u, rank);
         int k = w.k0 / prm.planes, pl = w.k0 - k * prm.planes;
         for (int j = w.k0; j < w.k1; ++j, ++n) {
-          const int r = n % C::kStagesRaw, s = n % C::kStages;
-          ok = mbar_wait(&bars->raw_empty[r], ((n / C::kStagesRaw) & 1) ^ 1);
-          if (!ok) break;
-          mbar_arrive_expect_tx(&bars->raw_full[r], kCodeBytes);
-          tma_load_2d(raws + (size_t)r * kRawBytes, &map_codes, w.i0, k * kTokens, &bars->raw_full[r]);
+          const int s = n % C::kStages;
           ok = mbar_wait(&bars->empty[s], ((n / C::kStages) & 1) ^ 1);
           if (!ok) break;
           if (rank == 0) mbar_arrive_expect_tx(&bars->full[s], PAIR * C::kBytesB);
@@ -281,7 +277,6 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
       // copies still in flight must land before the block may exit
       for (uint32_t m = n > (uint32_t)C::kStages ? n - C::kStages : 0; m < n; ++m)
         (void)mbar_wait(&bars->empty[m % C::kStages], (m / C::kStages) & 1);
-      if (!ok) (void)mbar_wait(&bars->raw_full[n % C::kStagesRaw], (n / C::kStagesRaw) & 1);
     }
     __syncwarp();
   } else if (warp == 1) {
@@ -393,10 +388,12 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
       if (lane == 0) arrive_first<PAIR>(&bars->full[s]);
     }
   } else {
-    // ---------------- scales: a lane copies the words of two tokens; words past the last token are zero
-    // (their codes are zero as well), the copies' arrival is counted on the stage's barrier
+    // ---------------- codes by TMA, and their scales: a lane copies the words of two tokens; words past the last
+    // token are zero (their codes are zero as well), the copies' arrival is counted on the stage's barrier.
+    // A warp of its own, so that codes are asked for as soon as the converters have room, whatever dY waits for.
     uint32_t n = 0;
     bool ok = true;
+    const bool leader = elect_one();
     for (int u = first_unit; u < units && ok; u += unit_step) {
       const Unit w = unit_of<N, PAIR>(prm, u, rank);
       // (the second block of a pair may have no inputs at all: its results are not stored)
@@ -406,6 +403,11 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
         const int r = n % C::kStagesRaw;
         ok = __all_sync(0xffffffffu, mbar_wait(&bars->raw_empty[r], ((n / C::kStagesRaw) & 1) ^ 1));
         if (!ok) break;
+        if (leader) {
+          mbar_arrive_expect_tx(&bars->raw_full[r], kCodeBytes);
+          tma_load_2d(raws + (size_t)r * kRawBytes, &map_codes, w.i0, k * kTokens, &bars->raw_full[r]);
+        }
+        __syncwarp();
         const uint32_t dst = smem_u32(raws + (size_t)r * kRawBytes + kCodeBytes);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -420,7 +422,11 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
         if (++pl == prm.planes) { pl = 0; ++k; }
       }
     }
-    asm volatile("cp.async.wait_all;" ::: "memory");     // nothing of this thread's is in flight at exit
+    // nothing may be in flight when the block exits: the codes of every step have to have landed
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    for (uint32_t m = n > (uint32_t)C::kStagesRaw ? n - C::kStagesRaw : 0; m < n; ++m)
+      (void)mbar_wait(&bars->raw_full[m % C::kStagesRaw], (m / C::kStagesRaw) & 1);
+    __syncwarp();
   }
 
   tc_fence_before();
