@@ -34,8 +34,10 @@ struct Act8 {
   uint8_t* scales;
 };
 
-// ---- 8 elements <-> floats.  VEC: rows start on 16-byte boundaries and cols is a multiple of 8, so a
-// chunk is whole or absent; otherwise elements are moved one by one up to the row's end.
+// ---- 8 elements of a row per thread.  VEC (rows start on 16-byte boundaries and cols is a multiple of 8):
+// eight neighbours, moved 16 bytes at a time, a chunk being whole or absent.  Otherwise (any alignment): eight
+// elements a multiple of 32 apart, so that the lanes of a warp touch neighbours and every group of 32 lies across
+// one warp; moved one by one.
 __device__ __forceinline__ float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -79,36 +81,43 @@ template <> struct Raw8<float> {
   }
 };
 
-// Elements c*8 .. c*8+7 of a row, zeros past its end.
+template <bool VEC>
+struct Place {
+  int first, step;
+  // chunk k of thread t when `width` threads (not VEC: a multiple of 32) share a row
+  __device__ __forceinline__ Place(int t, int width, int k)
+      : first(VEC ? (t + k * width) * 8 : k * width * 8 + t), step(VEC ? 1 : width) {}
+  __device__ __forceinline__ int at(int j) const { return first + j * step; }
+};
+
+// The elements, zeros past the row's end.
 template <typename T, bool VEC>
-__device__ __forceinline__ Raw8<T> load_chunk(const T* row, int c, int cols) {
+__device__ __forceinline__ Raw8<T> load_chunk(const T* row, const Place<VEC>& p, int cols) {
   Raw8<T> r;
-  const int j = c * 8;
   if constexpr (VEC) {
-    if (j < cols) r.load(row + j);
+    if (p.first < cols) r.load(row + p.first);
     else r.zero();
   } else {
     float v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = j + i < cols ? to_float(row[j + i]) : 0.f;
+    for (int j = 0; j < 8; ++j) v[j] = p.at(j) < cols ? to_float(row[p.at(j)]) : 0.f;
     r.put(v);      // exact: the values have T's precision
   }
   return r;
 }
 
 template <typename T, bool VEC>
-__device__ __forceinline__ void store_chunk(T* row, int c, int cols, const float (&v)[8]) {
-  const int j = c * 8;
+__device__ __forceinline__ void store_chunk(T* row, const Place<VEC>& p, int cols, const float (&v)[8]) {
   if constexpr (VEC) {
-    if (j < cols) {
+    if (p.first < cols) {
       Raw8<T> r;
       r.put(v);
-      r.store(row + j);
+      r.store(row + p.first);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (j + i < cols) row[j + i] = from_float<T>(v[i]);
+    for (int j = 0; j < 8; ++j)
+      if (p.at(j) < cols) row[p.at(j)] = from_float<T>(v[j]);
   }
 }
 
@@ -118,21 +127,25 @@ struct ParamVec {
   int is_bf16;
   int vec;             // 16-byte aligned and a multiple of 8 long
 };
-__device__ __forceinline__ void load_param(const ParamVec& w, int c, int cols, float none, float (&v)[8]) {
-  const int j = c * 8;
-  if (!w.p || j >= cols) {
+template <bool VEC>
+__device__ __forceinline__ void load_param(const ParamVec& w, const Place<VEC>& p, int cols, float none, float (&v)[8]) {
+  if (!w.p) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = none;
-  } else if (w.vec) {
-    if (w.is_bf16) { Raw8<bf16> r; r.load(static_cast<const bf16*>(w.p) + j); r.get(v); }
-    else { Raw8<float> r; r.load(static_cast<const float*>(w.p) + j); r.get(v); }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      v[i] = none;
-      if (j + i < cols)
-        v[i] = w.is_bf16 ? to_float(static_cast<const bf16*>(w.p)[j + i]) : static_cast<const float*>(w.p)[j + i];
+    for (int j = 0; j < 8; ++j) v[j] = none;
+    return;
+  }
+  if constexpr (VEC) {
+    if (w.vec && p.first < cols) {
+      if (w.is_bf16) { Raw8<bf16> r; r.load(static_cast<const bf16*>(w.p) + p.first); r.get(v); }
+      else { Raw8<float> r; r.load(static_cast<const float*>(w.p) + p.first); r.get(v); }
+      return;
     }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    v[j] = none;
+    if (p.at(j) < cols)
+      v[j] = w.is_bf16 ? to_float(static_cast<const bf16*>(w.p)[p.at(j)]) : static_cast<const float*>(w.p)[p.at(j)];
   }
 }
 
@@ -145,7 +158,7 @@ __device__ __forceinline__ void round_to(float (&v)[8]) {
   }
 }
 
-// ---- encode: the four lanes of an aligned quad hold one group, 8 values each.  All 32 lanes call.
+// ---- encode
 __device__ __forceinline__ uint32_t act8_scale_byte(uint32_t amax_bits) {
   // 127 * 2^e = 1.984375 * 2^(e+6): adding 2^17 - 1 carries into the exponent when the mantissa is above that
   const uint32_t k = (amax_bits + 0x1FFFFu) >> 23;
@@ -155,52 +168,104 @@ __device__ __forceinline__ float act8_scale(uint32_t byte) {
   return byte == 255u ? __uint_as_float(0x7FC00000u) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
 }
 
-__device__ __forceinline__ uint2 act8_encode(const float (&v)[8], uint32_t* byte_out) {
-  uint32_t m = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);   // NaN and Inf compare above all else
-  m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-  m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-  const uint32_t byte = act8_scale_byte(m);
-  *byte_out = byte;
-  const float inv = __uint_as_float((254u - byte) << 23);        // 2^-e, exact (byte <= 249 or 255)
-  const float top = byte == 249u ? 63.f : 127.f;                 // 64 * 2^122 is past the largest float
-  uint32_t q[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i)                                    // 1.5 * 2^23: rint in the low byte
-    q[i] = __float_as_uint(fminf(fmaxf(v[i] * inv, -top), top) + 12582912.f);
-  uint2 r;
-  r.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
-  r.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
-  if (byte == 255u) r = make_uint2(0, 0);
-  return r;
+// rint(v * 2^-e) as an int8 in the low byte (1.5 * 2^23 puts it there; the product is exact)
+__device__ __forceinline__ uint32_t act8_code(float v, float inv) { return __float_as_uint(fmaf(v, inv, 12582912.f)); }
+__device__ __forceinline__ float act8_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+// Codes at e = 122 end at +-63 (64 * 2^122 is no float): the value cut to that.
+__device__ __forceinline__ float act8_cut(float v) {
+  const float top = 63.f * 5.316911983139664e36f;     // 63 * 2^122
+  return fminf(fmaxf(v, -top), top);
 }
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }   // NaN and Inf on top
 
-// Codes and scale of chunk c of a row; the lane of the row's last group also clears the scales' padding.
-__device__ __forceinline__ void act8_put(uint8_t* codes_row, uint8_t* scales_row, int c, int groups, const float (&v)[8],
-                                         bool valid) {
-  uint32_t byte;
-  const uint2 q = act8_encode(v, &byte);
-  if (!valid) return;
-  *reinterpret_cast<uint2*>(codes_row + (size_t)c * 8) = q;
-  if ((c & 3) == 0) {
-    const int g = c >> 2;
-    scales_row[g] = static_cast<uint8_t>(byte);
-    if (g == groups - 1)
-      for (int i = groups; i & 3; ++i) scales_row[i] = 0;
+// The values at `p` (zeros past the row's end) into the checkpoint's row.  All 32 lanes call; `valid`: this
+// thread's chunk belongs to a row.  VEC: a group lies across an aligned quad of lanes.  The lane of the row's last
+// group also clears the scales' padding.
+template <bool VEC>
+__device__ __forceinline__ void act8_put(uint8_t* codes_row, uint8_t* scales_row, const Place<VEC>& p, int groups,
+                                         const float (&v)[8], bool valid) {
+  if constexpr (VEC) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[i]));
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+    const uint32_t byte = act8_scale_byte(m);
+    const float inv = act8_inverse(byte);
+    uint32_t q[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = act8_code(v[i], inv);
+    if (byte == 249u) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) q[i] = act8_code(act8_cut(v[i]), inv);
+    }
+    uint2 r;
+    r.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+    r.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
+    if (byte == 255u) r = make_uint2(0, 0);
+    if (!valid || p.first >= groups * 32) return;
+    *reinterpret_cast<uint2*>(codes_row + p.first) = r;
+    if ((p.first & 31) == 0) {
+      const int g = p.first >> 5;
+      scales_row[g] = static_cast<uint8_t>(byte);
+      if (g == groups - 1)
+        for (int i = groups; i & 3; ++i) scales_row[i] = 0;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t byte = act8_scale_byte(__reduce_max_sync(0xffffffffu, magnitude(v[j])));
+      const uint32_t q = byte == 255u ? 0u : act8_code(byte == 249u ? act8_cut(v[j]) : v[j], act8_inverse(byte));
+      const int i = p.at(j), g = i >> 5;
+      if (!valid || g >= groups) continue;
+      codes_row[i] = static_cast<uint8_t>(q);
+      if ((i & 31) == 0) {
+        scales_row[g] = static_cast<uint8_t>(byte);
+        if (g == groups - 1)
+          for (int k = groups; k & 3; ++k) scales_row[k] = 0;
+      }
+    }
   }
 }
 
 // ---- decode
-__device__ __forceinline__ void act8_decode(uint2 q, uint32_t byte, float (&v)[8]) {
-  const float s = act8_scale(byte);
-  const uint32_t a = q.x ^ 0x80808080u, b = q.y ^ 0x80808080u;   // code + 128 as an unsigned byte
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {                                 // 2^23 + (code + 128) by its bits, minus the offset: exact
-    v[i] = (__uint_as_float(__byte_perm(a, 0x4B000000u, 0x7440 + i)) - 8388736.f) * s;
-    v[4 + i] = (__uint_as_float(__byte_perm(b, 0x4B000000u, 0x7440 + i)) - 8388736.f) * s;
+// Codes and scales as they lie in memory.
+template <bool VEC> struct RawAct8;
+template <> struct RawAct8<true> {
+  uint2 q;
+  uint32_t byte;
+  __device__ __forceinline__ void load(const uint8_t* codes_row, const uint8_t* scales_row, const Place<true>& p, int groups) {
+    q = make_uint2(0, 0);
+    byte = 127;
+    if (p.first < groups * 32) {
+      q = *reinterpret_cast<const uint2*>(codes_row + p.first);
+      byte = scales_row[p.first >> 5];
+    }
   }
-}
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    const float s = act8_scale(byte);
+    const uint32_t a = q.x ^ 0x80808080u, b = q.y ^ 0x80808080u;   // code + 128 as an unsigned byte
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {                                 // 2^23 + (code + 128) by its bits, minus the offset: exact
+      v[i] = (__uint_as_float(__byte_perm(a, 0x4B000000u, 0x7440 + i)) - 8388736.f) * s;
+      v[4 + i] = (__uint_as_float(__byte_perm(b, 0x4B000000u, 0x7440 + i)) - 8388736.f) * s;
+    }
+  }
+};
+template <> struct RawAct8<false> {
+  float v_[8];
+  __device__ __forceinline__ void load(const uint8_t* codes_row, const uint8_t* scales_row, const Place<false>& p, int groups) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int i = p.at(j);
+      v_[j] = i < groups * 32 ? (float)static_cast<int8_t>(codes_row[i]) * act8_scale(scales_row[i >> 5]) : 0.f;
+    }
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = v_[j];
+  }
+};
 
 // ---- division by a number fixed per launch, for 0 <= n < 2^31
 struct FastDiv {

@@ -10,16 +10,20 @@ namespace act8 {
 constexpr int kThreads = 256;
 constexpr int kPer = 4;              // chunks per thread, loaded before any is worked on
 
-// A launch covers the chunks 0 .. n-1 of `rows` rows, `per_row` (a multiple of 4) chunks each; n < 2^31.
+// A launch covers the chunks 0 .. n-1 of its rows, `per_row` each (VEC: 4 a group; otherwise 32 for every 256
+// elements, one per lane); n < 2^31.
 struct Flat {
   uint32_t n;
   int cols, groups, scale_pitch;
   FastDiv per_row;
 };
 
-__device__ __forceinline__ void split(const Flat& f, uint32_t i, uint32_t* row, int* c) {
+template <bool VEC>
+__device__ __forceinline__ Place<VEC> split(const Flat& f, uint32_t i, uint32_t* row) {
   *row = f.per_row.div(i);
-  *c = static_cast<int>(i - *row * f.per_row.d);
+  const int c = static_cast<int>(i - *row * f.per_row.d);
+  if constexpr (VEC) return Place<VEC>(c, 0, 0);
+  else return Place<VEC>(c & 31, 32, c >> 5);
 }
 
 template <typename T, bool VEC>
@@ -27,44 +31,43 @@ __global__ void __launch_bounds__(kThreads) store_kernel(const T* __restrict__ x
   const uint32_t first = blockIdx.x * (kThreads * kPer) + threadIdx.x;
   Raw8<T> raw[kPer];
   uint32_t row[kPer];
-  int c[kPer];
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const uint32_t i = first + k * kThreads;
-    split(f, i < f.n ? i : 0u, &row[k], &c[k]);
-    if (i < f.n) raw[k] = load_chunk<T, VEC>(x + row[k] * ldx, c[k], f.cols);
+    const Place<VEC> p = split<VEC>(f, i < f.n ? i : 0u, &row[k]);
+    if (i < f.n) raw[k] = load_chunk<T, VEC>(x + row[k] * ldx, p, f.cols);
     else raw[k].zero();
   }
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     float v[8];
     raw[k].get(v);
-    act8_put(ck.codes + (size_t)row[k] * f.groups * 32, ck.scales + (size_t)row[k] * f.scale_pitch, c[k], f.groups, v,
-             first + k * kThreads < f.n);
+    const uint32_t i = first + k * kThreads;
+    const Place<VEC> p = split<VEC>(f, i < f.n ? i : 0u, &row[k]);
+    act8_put<VEC>(ck.codes + (size_t)row[k] * f.groups * 32, ck.scales + (size_t)row[k] * f.scale_pitch, p, f.groups, v,
+                  i < f.n);
   }
 }
 
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads) load_kernel(Act8 ck, T* __restrict__ out, long long ldo, Flat f) {
   const uint32_t first = blockIdx.x * (kThreads * kPer) + threadIdx.x;
-  uint2 q[kPer];
-  uint32_t byte[kPer], row[kPer];
-  int c[kPer];
+  RawAct8<VEC> q[kPer];
+  uint32_t row[kPer];
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const uint32_t i = first + k * kThreads;
-    split(f, i < f.n ? i : 0u, &row[k], &c[k]);
-    if (i < f.n) {
-      q[k] = *reinterpret_cast<const uint2*>(ck.codes + (size_t)row[k] * f.groups * 32 + (size_t)c[k] * 8);
-      byte[k] = ck.scales[(size_t)row[k] * f.scale_pitch + (c[k] >> 2)];
-    }
+    const Place<VEC> p = split<VEC>(f, i < f.n ? i : 0u, &row[k]);
+    if (i < f.n) q[k].load(ck.codes + (size_t)row[k] * f.groups * 32, ck.scales + (size_t)row[k] * f.scale_pitch, p, f.groups);
   }
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
-    if (first + k * kThreads >= f.n) continue;
+    const uint32_t i = first + k * kThreads;
+    if (i >= f.n) continue;
+    const Place<VEC> p = split<VEC>(f, i, &row[k]);
     float v[8];
-    act8_decode(q[k], byte[k], v);
-    store_chunk<T, VEC>(out + row[k] * ldo, c[k], f.cols, v);
+    q[k].get(v);
+    store_chunk<T, VEC>(out + row[k] * ldo, p, f.cols, v);
   }
 }
 
@@ -99,74 +102,91 @@ __global__ void __launch_bounds__(kThreads) gelu_forward_kernel(const T* __restr
   const uint32_t first = blockIdx.x * (kThreads * kPer) + threadIdx.x;
   Raw8<T> raw[kPer];
   uint32_t row[kPer];
-  int c[kPer];
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const uint32_t i = first + k * kThreads;
-    split(f, i < f.n ? i : 0u, &row[k], &c[k]);
-    if (i < f.n) raw[k] = load_chunk<T, VEC>(x + row[k] * ldx, c[k], f.cols);
+    const Place<VEC> p = split<VEC>(f, i < f.n ? i : 0u, &row[k]);
+    if (i < f.n) raw[k] = load_chunk<T, VEC>(x + row[k] * ldx, p, f.cols);
     else raw[k].zero();
   }
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
-    const bool valid = first + k * kThreads < f.n;
+    const uint32_t i = first + k * kThreads;
+    const bool valid = i < f.n;
+    const Place<VEC> p = split<VEC>(f, valid ? i : 0u, &row[k]);
+    const size_t code_row = (size_t)row[k] * f.groups * 32, scale_row = (size_t)row[k] * f.scale_pitch;
     float z[8], b[8];
     raw[k].get(z);
     if (bias.p) {
-      load_param(bias, c[k], f.cols, 0.f, b);
+      load_param<VEC>(bias, p, f.cols, 0.f, b);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) z[i] += b[i];
+      for (int j = 0; j < 8; ++j) z[j] += b[j];
     }
-    if (ck_x.codes)
-      act8_put(ck_x.codes + (size_t)row[k] * f.groups * 32, ck_x.scales + (size_t)row[k] * f.scale_pitch, c[k],
-               f.groups, z, valid);
+    if (ck_x.codes) act8_put<VEC>(ck_x.codes + code_row, ck_x.scales + scale_row, p, f.groups, z, valid);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] = gelu<T, APPROX>(z[i]);
-    if (valid) store_chunk<T, VEC>(y + row[k] * ldy, c[k], f.cols, z);
+    for (int j = 0; j < 8; ++j) z[j] = gelu<T, APPROX>(z[j]);
+    if (valid) store_chunk<T, VEC>(y + row[k] * ldy, p, f.cols, z);
     if (ck_y.codes) {
       round_to<T>(z);                     // the checkpoint holds y as it is stored
-      act8_put(ck_y.codes + (size_t)row[k] * f.groups * 32, ck_y.scales + (size_t)row[k] * f.scale_pitch, c[k],
-               f.groups, z, valid);
+      act8_put<VEC>(ck_y.codes + code_row, ck_y.scales + scale_row, p, f.groups, z, valid);
     }
   }
 }
 
-// ---- column kernels: a thread owns the 8 columns of one chunk and walks over rows; its sums stay in
-// registers.  A block has 256 / lanes rows side by side, `lanes` (a power of two) chunks wide.
+// ---- column kernels: a thread owns 8 columns and walks over rows; its sums stay in registers.  A block has
+// 256 / lanes rows side by side, `lanes` (a power of two; not VEC: 32) chunks wide.  Rows are taken kAhead at a
+// time, loads first.
+constexpr int kAhead = 4;
 struct Columns {
   long long rows;
-  int cols, chunks, lanes_log2;
-  float* partials;           // [gridDim.y][chunks * 8], or null
+  int chunks, lanes_log2;    // chunks of a row: VEC 4 a group, otherwise 32 for every 256 elements
+  int width;                 // of the partial sums
+  float* partials;           // [gridDim.y][width], or null
 };
 
 template <class Op>
 __global__ void __launch_bounds__(kThreads) column_kernel(Op op, Columns g) {
+  constexpr bool VEC = Op::kVec;
   const int lanes = 1 << g.lanes_log2, side = kThreads >> g.lanes_log2;
-  const int rl = threadIdx.x >> g.lanes_log2;
-  const int c = blockIdx.x * lanes + (threadIdx.x & (lanes - 1));
+  const int rl = threadIdx.x >> g.lanes_log2, lane = threadIdx.x & (lanes - 1);
+  const int c = blockIdx.x * lanes + lane;
+  const Place<VEC> p = VEC ? Place<VEC>(c, 0, 0) : Place<VEC>(lane, 32, blockIdx.x);
   float acc[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) acc[i] = 0.f;
   if (c < g.chunks) {
-    op.begin(c);
-    for (long long r = (long long)blockIdx.y * side + rl; r < g.rows; r += (long long)gridDim.y * side) op.row(r, c, acc);
+    op.begin(p);
+    const long long step = (long long)gridDim.y * side;
+    for (long long r = (long long)blockIdx.y * side + rl; r < g.rows; r += step * kAhead) {
+      typename Op::In in[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (r + k * step < g.rows) op.load(r + k * step, p, in[k]);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (r + k * step < g.rows) op.row(r + k * step, p, in[k], acc);
+    }
   }
   if (!g.partials) return;
   __shared__ float sums[kThreads * 9];       // 9 floats apart: the threads of a column group spread over the banks
 #pragma unroll
   for (int i = 0; i < 8; ++i) sums[threadIdx.x * 9 + i] = acc[i];
   __syncthreads();
+  float* out = g.partials + (size_t)blockIdx.y * g.width;
   for (int j = threadIdx.x; j < lanes * 8; j += kThreads) {
-    const int cc = blockIdx.x * lanes + (j >> 3);
-    if (cc >= g.chunks) continue;
+    // column j of the block: element j / lanes of lane j % lanes, or (VEC) element j % 8 of lane j / 8
+    const int l = VEC ? j >> 3 : j & (lanes - 1), e = VEC ? j & 7 : j >> g.lanes_log2;
+    const int col = blockIdx.x * lanes * 8 + j;
+    if (col >= g.width) continue;
     float s = 0.f;
-    for (int k = 0; k < side; ++k) s += sums[(k * lanes + (j >> 3)) * 9 + (j & 7)];
-    g.partials[(size_t)blockIdx.y * g.chunks * 8 + (size_t)cc * 8 + (j & 7)] = s;
+    for (int k = 0; k < side; ++k) s += sums[(k * lanes + l) * 9 + e];
+    out[col] = s;
   }
 }
 
-template <typename T, bool VEC, int APPROX>
+template <typename T, bool VEC, int APPROX, bool CK>
 struct GeluBackward {
+  static constexpr bool kVec = VEC;
   const T* dy; long long lddy;
   const T* x; long long ldx;
   ParamVec bias;
@@ -174,15 +194,25 @@ struct GeluBackward {
   int cols, groups, scale_pitch;
   T* dx; long long lddx;
   float b[8];
-  __device__ __forceinline__ void begin(int c) { load_param(bias, c, cols, 0.f, b); }
-  __device__ __forceinline__ void row(long long r, int c, float (&acc)[8]) {
+  struct In {
+    Raw8<T> dy, x;
+    RawAct8<VEC> q;
+  };
+  __device__ __forceinline__ void begin(const Place<VEC>& p) {
+    if (!CK) load_param<VEC>(bias, p, cols, 0.f, b);
+  }
+  __device__ __forceinline__ void load(long long r, const Place<VEC>& p, In& in) const {
+    in.dy = load_chunk<T, VEC>(dy + r * lddy, p, cols);
+    if constexpr (CK) in.q.load(ck.codes + (size_t)r * groups * 32, ck.scales + (size_t)r * scale_pitch, p, groups);
+    else in.x = load_chunk<T, VEC>(x + r * ldx, p, cols);
+  }
+  __device__ __forceinline__ void row(long long r, const Place<VEC>& p, const In& in, float (&acc)[8]) const {
     float g[8], z[8];
-    load_chunk<T, VEC>(dy + r * lddy, c, cols).get(g);
-    if (ck.codes) {
-      act8_decode(*reinterpret_cast<const uint2*>(ck.codes + (size_t)r * groups * 32 + (size_t)c * 8),
-                  ck.scales[(size_t)r * scale_pitch + (c >> 2)], z);
+    in.dy.get(g);
+    if constexpr (CK) {
+      in.q.get(z);
     } else {
-      load_chunk<T, VEC>(x + r * ldx, c, cols).get(z);
+      in.x.get(z);
 #pragma unroll
       for (int i = 0; i < 8; ++i) z[i] += b[i];
     }
@@ -191,18 +221,23 @@ struct GeluBackward {
       g[i] *= gelu_slope<T, APPROX>(z[i]);
       acc[i] += g[i];
     }
-    store_chunk<T, VEC>(dx + r * lddx, c, cols, g);
+    store_chunk<T, VEC>(dx + r * lddx, p, cols, g);
   }
 };
 
 template <typename T, bool VEC>
 struct ColumnSum {
+  static constexpr bool kVec = VEC;
   const T* x; long long ldx;
   int cols;
-  __device__ __forceinline__ void begin(int) {}
-  __device__ __forceinline__ void row(long long r, int c, float (&acc)[8]) {
+  struct In { Raw8<T> x; };
+  __device__ __forceinline__ void begin(const Place<VEC>&) {}
+  __device__ __forceinline__ void load(long long r, const Place<VEC>& p, In& in) const {
+    in.x = load_chunk<T, VEC>(x + r * ldx, p, cols);
+  }
+  __device__ __forceinline__ void row(long long, const Place<VEC>&, const In& in, float (&acc)[8]) const {
     float v[8];
-    load_chunk<T, VEC>(x + r * ldx, c, cols).get(v);
+    in.x.get(v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i] += v[i];
   }
@@ -210,39 +245,38 @@ struct ColumnSum {
 
 }  // namespace act8
 
-__global__ void __launch_bounds__(256) finish_columns_kernel(const float* __restrict__ partials, int parts, int sums,
-                                                             long long width, long long cols, void* out0, void* out1,
-                                                             int gbf16) {
-  __shared__ float s[8][32];
-  const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
+// A block adds 32 columns of one sum, a warp taking every kFinishWarps-th part; the warps' sums are added in order.
+constexpr int kFinishWarps = 16;
+__global__ void __launch_bounds__(32 * kFinishWarps) finish_columns_kernel(const float* __restrict__ partials, int parts,
+                                                                           int sums, long long width, long long cols,
+                                                                           void* out0, void* out1, int gbf16) {
+  __shared__ float s[kFinishWarps][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = blockIdx.y;
   const long long col = (long long)blockIdx.x * 32 + lane;
-  for (int k = 0; k < sums; ++k) {
-    void* out = k ? out1 : out0;
-    if (!out) continue;
-    float v = 0.f;
-    if (col < cols) {
-      const float* p = partials + (size_t)k * width + col;
+  void* out = k ? out1 : out0;
+  if (!out) return;
+  float v = 0.f;
+  if (col < cols) {
+    const float* p = partials + (size_t)k * width + col;
+    const size_t step = (size_t)sums * width;
 #pragma unroll 8
-      for (int b = slice; b < parts; b += 8) v += p[(size_t)b * sums * width];
-    }
-    s[slice][lane] = v;
-    __syncthreads();
-    if (slice == 0 && col < cols) {
-      v = 0.f;
+    for (int b = warp; b < parts; b += kFinishWarps) v += p[b * step];
+  }
+  s[warp][lane] = v;
+  __syncthreads();
+  if (warp == 0 && col < cols) {
+    v = 0.f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v += s[j][lane];
-      if (gbf16) static_cast<bf16*>(out)[col] = __float2bfloat16_rn(v);
-      else static_cast<float*>(out)[col] = v;
-    }
-    __syncthreads();
+    for (int j = 0; j < kFinishWarps; ++j) v += s[j][lane];
+    if (gbf16) static_cast<bf16*>(out)[col] = __float2bfloat16_rn(v);
+    else static_cast<float*>(out)[col] = v;
   }
 }
 
 cudaError_t launch_finish_columns(const float* partials, int parts, int sums, long long width, long long cols,
                                   void* out0, void* out1, int gdtype, cudaStream_t st) {
-  const long long blocks = (cols + 31) / 32;
-  finish_columns_kernel<<<(unsigned)blocks, 256, 0, st>>>(partials, parts, sums, width, cols, out0, out1,
-                                                          gdtype == FA_BF16);
+  const dim3 grid((unsigned)((cols + 31) / 32), sums);
+  finish_columns_kernel<<<grid, 32 * kFinishWarps, 0, st>>>(partials, parts, sums, width, cols, out0, out1, gdtype == FA_BF16);
   return cudaGetLastError();
 }
 
@@ -251,8 +285,8 @@ namespace {
 
 // One launch per piece of at most 2^30 chunks (or one row, which has fewer than 2^28).
 template <class Launch>
-cudaError_t for_flat(long long rows, long long cols, Launch launch) {
-  const long long groups = act8_groups(cols), per_row = groups * 4;
+cudaError_t for_flat(bool vec, long long rows, long long cols, Launch launch) {
+  const long long groups = act8_groups(cols), per_row = vec ? groups * 4 : (groups + 7) / 8 * 32;
   const long long piece = (1LL << 30) / per_row;
   for (long long r0 = 0; r0 < rows; r0 += piece) {
     const long long n = rows - r0 < piece ? rows - r0 : piece;
@@ -273,7 +307,7 @@ cudaError_t for_flat(long long rows, long long cols, Launch launch) {
 template <typename T>
 cudaError_t store_t(Mat x, long long rows, long long cols, void* ck, cudaStream_t st) {
   const bool vec = mat_vec<T>(x, cols);
-  return for_flat(rows, cols, [&](unsigned blocks, const act8::Flat& f, long long r0) {
+  return for_flat(vec, rows, cols, [&](unsigned blocks, const act8::Flat& f, long long r0) {
     if (vec) act8::store_kernel<T, true><<<blocks, act8::kThreads, 0, st>>>(row_of<T>(x, r0), x.ld, act8_at(ck, rows, cols, r0), f);
     else act8::store_kernel<T, false><<<blocks, act8::kThreads, 0, st>>>(row_of<T>(x, r0), x.ld, act8_at(ck, rows, cols, r0), f);
   });
@@ -281,7 +315,7 @@ cudaError_t store_t(Mat x, long long rows, long long cols, void* ck, cudaStream_
 template <typename T>
 cudaError_t load_t(const void* ck, long long rows, long long cols, Mat out, cudaStream_t st) {
   const bool vec = mat_vec<T>(out, cols);
-  return for_flat(rows, cols, [&](unsigned blocks, const act8::Flat& f, long long r0) {
+  return for_flat(vec, rows, cols, [&](unsigned blocks, const act8::Flat& f, long long r0) {
     if (vec) act8::load_kernel<T, true><<<blocks, act8::kThreads, 0, st>>>(act8_at(ck, rows, cols, r0), row_of<T>(out, r0), out.ld, f);
     else act8::load_kernel<T, false><<<blocks, act8::kThreads, 0, st>>>(act8_at(ck, rows, cols, r0), row_of<T>(out, r0), out.ld, f);
   });
@@ -290,7 +324,7 @@ template <typename T, bool VEC, int APPROX>
 cudaError_t gelu_forward_t(Mat x, long long rows, long long cols, Param bias, Mat y, void* ck_x, void* ck_y,
                            cudaStream_t st) {
   const ParamVec b = param_vec(bias, cols);
-  return for_flat(rows, cols, [&](unsigned blocks, const act8::Flat& f, long long r0) {
+  return for_flat(VEC, rows, cols, [&](unsigned blocks, const act8::Flat& f, long long r0) {
     act8::gelu_forward_kernel<T, VEC, APPROX><<<blocks, act8::kThreads, 0, st>>>(
         row_of<T>(x, r0), x.ld, b, row_of<T>(y, r0), y.ld, act8_at(ck_x, rows, cols, r0),
         act8_at(ck_y, rows, cols, r0), f);
@@ -311,13 +345,15 @@ cudaError_t gelu_forward_d(Mat x, long long rows, long long cols, Param bias, in
 struct ColumnGrid {
   int lanes_log2;
   unsigned x, y;
-  long long chunks;
+  long long chunks, width;
 };
-ColumnGrid column_grid(long long rows, long long cols) {
+ColumnGrid column_grid(bool vec, long long rows, long long cols) {
   ColumnGrid g{};
-  g.chunks = act8_groups(cols) * 4;
+  const long long groups = act8_groups(cols);
+  g.width = groups * 32;
+  g.chunks = vec ? groups * 4 : (groups + 7) / 8 * 32;
   g.lanes_log2 = 5;
-  while (g.lanes_log2 > 2 && (1LL << (g.lanes_log2 - 1)) >= g.chunks) --g.lanes_log2;
+  while (vec && g.lanes_log2 > 2 && (1LL << (g.lanes_log2 - 1)) >= g.chunks) --g.lanes_log2;
   const long long lanes = 1LL << g.lanes_log2, side = act8::kThreads / lanes;
   const long long x = (g.chunks + lanes - 1) / lanes;
   long long y = (4LL * sm_count() + x - 1) / x;
@@ -332,12 +368,12 @@ ColumnGrid column_grid(long long rows, long long cols) {
 template <class Op>
 cudaError_t run_columns(const Op& op, long long rows, long long cols, void* out, int gdtype, float* partials,
                         cudaStream_t st) {
-  const ColumnGrid g = column_grid(rows, cols);
+  const ColumnGrid g = column_grid(Op::kVec, rows, cols);
   if (rows > 0) {
     act8::Columns p{};
     p.rows = rows;
-    p.cols = static_cast<int>(cols);
     p.chunks = static_cast<int>(g.chunks);
+    p.width = static_cast<int>(g.width);
     p.lanes_log2 = g.lanes_log2;
     p.partials = out ? partials : nullptr;
     act8::column_kernel<Op><<<dim3(g.x, g.y), act8::kThreads, 0, st>>>(op, p);
@@ -345,32 +381,42 @@ cudaError_t run_columns(const Op& op, long long rows, long long cols, void* out,
     if (e != cudaSuccess) return e;
   }
   if (!out) return cudaSuccess;
-  return launch_finish_columns(partials, rows > 0 ? (int)g.y : 0, 1, g.chunks * 8, cols, out, nullptr, gdtype, st);
+  return launch_finish_columns(partials, rows > 0 ? (int)g.y : 0, 1, g.width, cols, out, nullptr, gdtype, st);
 }
 
-template <typename T, bool VEC, int APPROX>
-cudaError_t gelu_backward_t(Mat dy, Mat x, Param bias, const void* ck, long long rows, long long cols, Mat dx,
-                            void* dbias, int gdtype, float* partials, cudaStream_t st) {
-  act8::GeluBackward<T, VEC, APPROX> op{};
-  op.dy = row_of<T>(dy, 0); op.lddy = dy.ld;
-  op.x = row_of<T>(x, 0); op.ldx = x.ld;
-  op.bias = param_vec(bias, cols);
-  op.ck = act8_at(ck, rows, cols, 0);
-  op.cols = static_cast<int>(cols);
-  op.groups = static_cast<int>(act8_groups(cols));
-  op.scale_pitch = static_cast<int>(act8_scale_pitch(cols));
-  op.dx = row_of<T>(dx, 0); op.lddx = dx.ld;
-  return run_columns(op, rows, cols, dbias, gdtype, partials, st);
+struct GeluBackwardArgs {
+  Mat dy, x;
+  Param bias;
+  const void* ck;
+  long long rows, cols;
+  Mat dx;
+  void* dbias;
+  int gdtype;
+  float* partials;
+};
+template <typename T, bool VEC, int APPROX, bool CK>
+cudaError_t gelu_backward_t(const GeluBackwardArgs& a, cudaStream_t st) {
+  act8::GeluBackward<T, VEC, APPROX, CK> op{};
+  op.dy = row_of<T>(a.dy, 0); op.lddy = a.dy.ld;
+  op.x = row_of<T>(a.x, 0); op.ldx = a.x.ld;
+  op.bias = param_vec(a.bias, a.cols);
+  op.ck = act8_at(a.ck, a.rows, a.cols, 0);
+  op.cols = static_cast<int>(a.cols);
+  op.groups = static_cast<int>(act8_groups(a.cols));
+  op.scale_pitch = static_cast<int>(act8_scale_pitch(a.cols));
+  op.dx = row_of<T>(a.dx, 0); op.lddx = a.dx.ld;
+  return run_columns(op, a.rows, a.cols, a.dbias, a.gdtype, a.partials, st);
+}
+template <typename T, bool VEC>
+cudaError_t gelu_backward_v(const GeluBackwardArgs& a, int approx, cudaStream_t st) {
+  if (approx == kGeluTanh)
+    return a.ck ? gelu_backward_t<T, VEC, kGeluTanh, true>(a, st) : gelu_backward_t<T, VEC, kGeluTanh, false>(a, st);
+  return a.ck ? gelu_backward_t<T, VEC, kGeluErf, true>(a, st) : gelu_backward_t<T, VEC, kGeluErf, false>(a, st);
 }
 template <typename T>
-cudaError_t gelu_backward_d(Mat dy, Mat x, Param bias, const void* ck, long long rows, long long cols, int approx,
-                            Mat dx, void* dbias, int gdtype, float* partials, cudaStream_t st) {
-  const bool vec = mat_vec<T>(dy, cols) && mat_vec<T>(x, cols) && mat_vec<T>(dx, cols);
-  if (approx == kGeluTanh)
-    return vec ? gelu_backward_t<T, true, kGeluTanh>(dy, x, bias, ck, rows, cols, dx, dbias, gdtype, partials, st)
-               : gelu_backward_t<T, false, kGeluTanh>(dy, x, bias, ck, rows, cols, dx, dbias, gdtype, partials, st);
-  return vec ? gelu_backward_t<T, true, kGeluErf>(dy, x, bias, ck, rows, cols, dx, dbias, gdtype, partials, st)
-             : gelu_backward_t<T, false, kGeluErf>(dy, x, bias, ck, rows, cols, dx, dbias, gdtype, partials, st);
+cudaError_t gelu_backward_d(const GeluBackwardArgs& a, int approx, cudaStream_t st) {
+  const bool vec = mat_vec<T>(a.dy, a.cols) && mat_vec<T>(a.x, a.cols) && mat_vec<T>(a.dx, a.cols);
+  return vec ? gelu_backward_v<T, true>(a, approx, st) : gelu_backward_v<T, false>(a, approx, st);
 }
 template <typename T>
 cudaError_t column_sum_d(Mat x, long long rows, long long cols, void* out, int gdtype, float* partials,
@@ -397,14 +443,13 @@ cudaError_t launch_gelu_forward(Mat x, int dtype, long long rows, long long cols
                           : gelu_forward_d<float>(x, rows, cols, bias, approx, y, ck_x, ck_y, st);
 }
 size_t column_partials_bytes(long long rows, long long cols) {
-  const ColumnGrid g = column_grid(rows, cols);
-  return (size_t)g.y * g.chunks * 8 * sizeof(float);
+  const ColumnGrid v = column_grid(true, rows, cols), e = column_grid(false, rows, cols);   // known at the call
+  return (size_t)(v.y > e.y ? v.y : e.y) * v.width * sizeof(float);
 }
 cudaError_t launch_gelu_backward(Mat dy, Mat x, Param bias, const void* ck, int dtype, long long rows, long long cols,
                                  int approx, Mat dx, void* dbias, int gdtype, float* partials, cudaStream_t st) {
-  return dtype == FA_BF16
-             ? gelu_backward_d<bf16>(dy, x, bias, ck, rows, cols, approx, dx, dbias, gdtype, partials, st)
-             : gelu_backward_d<float>(dy, x, bias, ck, rows, cols, approx, dx, dbias, gdtype, partials, st);
+  const GeluBackwardArgs a{dy, x, bias, ck, rows, cols, dx, dbias, gdtype, partials};
+  return dtype == FA_BF16 ? gelu_backward_d<bf16>(a, approx, st) : gelu_backward_d<float>(a, approx, st);
 }
 cudaError_t launch_column_sum(Mat x, int dtype, long long rows, long long cols, void* out, int gdtype, float* partials,
                               cudaStream_t st) {

@@ -8,7 +8,6 @@
 namespace fa {
 
 // partials: [parts][sums][width] floats; out0 / out1 (null: not wanted) receive sum 0 / 1 of columns < cols.
-// A block adds 32 columns with 8 threads each; thread s takes the parts s, s + 8, ... in order.
 cudaError_t launch_finish_columns(const float* partials, int parts, int sums, long long width, long long cols,
                                   void* out0, void* out1, int gdtype, cudaStream_t st);
 

@@ -455,17 +455,18 @@ __global__ void __launch_bounds__(256) add_splits_kernel(const float* __restrict
 
 // dY as bf16 terms that add up to it exactly, rows of `pitch` elements: [planes][rows][pitch].  Terms are
 // cut off rather than rounded, so that no finite value becomes infinite; what is not finite is one term.
-template <typename T>
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ dy, long long ld, long long rows, int outs,
                                                    int pitch, int planes, bf16* __restrict__ out) {
-  const int chunks = pitch / 8;
-  const long long n = rows * chunks, plane = rows * pitch;
+  const int per_row = VEC ? pitch / 8 : (outs + 255) / 256 * 32;
+  const long long n = rows * per_row, plane = rows * pitch;
   for (long long j = (long long)blockIdx.x * 256 + threadIdx.x; j < n; j += (long long)gridDim.x * 256) {
-    const long long r = j / chunks;
-    const int c = static_cast<int>(j - r * chunks);
+    const long long r = j / per_row;
+    const int c = static_cast<int>(j - r * per_row);
+    const Place<VEC> p = VEC ? Place<VEC>(c, 0, 0) : Place<VEC>(c & 31, 32, c >> 5);
     float v[8];
-    load_chunk<T, false>(dy + r * ld, c, outs).get(v);
-    for (int p = 0; p < planes; ++p) {
+    load_chunk<T, VEC>(dy + r * ld, p, outs).get(v);
+    for (int q = 0; q < planes; ++q) {
       float term[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
@@ -473,9 +474,7 @@ __global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ dy, lon
         if (isnan(v[k])) term[k] = v[k];
         v[k] = isfinite(v[k]) ? v[k] - term[k] : 0.f;
       }
-      Raw8<bf16> o;
-      o.put(term);
-      o.store(out + p * plane + r * pitch + c * 8);
+      store_chunk<bf16, VEC>(out + q * plane + r * pitch, p, outs, term);
     }
   }
 }
@@ -551,13 +550,15 @@ cudaError_t launch_linear_weight_grad(Mat dy, int dtype, long long rows, long lo
   long long ld = dy.ld;
   if (!direct) {
     bf16* packed = static_cast<bf16*>(scratch);
-    const long long chunks = rows * (p.pitch / 8);
-    const long long want = (chunks + 255) / 256, most = 16LL * sm_count();
+    const bool vec = dtype == FA_F32 && mat_vec<float>(dy, outs);
+    const long long want = (rows * (vec ? p.pitch / 8 : (outs + 255) / 256 * 32) + 255) / 256, most = 16LL * sm_count();
     const unsigned grid = static_cast<unsigned>(want < most ? want : most);
-    if (dtype == FA_BF16)
-      wgrad::pack_kernel<bf16><<<grid, 256, 0, st>>>(row_of<bf16>(dy, 0), dy.ld, rows, (int)outs, p.pitch, p.planes, packed);
-    else
-      wgrad::pack_kernel<float><<<grid, 256, 0, st>>>(row_of<float>(dy, 0), dy.ld, rows, (int)outs, p.pitch, p.planes, packed);
+    auto go = [&](auto kernel, auto* src) {
+      kernel<<<grid, 256, 0, st>>>(src, dy.ld, rows, (int)outs, p.pitch, p.planes, packed);
+    };
+    if (dtype == FA_BF16) go(wgrad::pack_kernel<bf16, false>, row_of<const bf16>(dy, 0));
+    else if (vec) go(wgrad::pack_kernel<float, true>, row_of<const float>(dy, 0));
+    else go(wgrad::pack_kernel<float, false>, row_of<const float>(dy, 0));
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     base = packed;
