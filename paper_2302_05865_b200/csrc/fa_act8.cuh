@@ -34,6 +34,40 @@ struct Act8 {
   uint8_t* scales;
 };
 
+// Two floats in one 64-bit register: sm_100 works on both with one instruction.
+struct F2 {
+  unsigned long long v;
+};
+__device__ __forceinline__ F2 two(float lo, float hi) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ F2 two(float both) { return two(both, both); }
+__device__ __forceinline__ void apart(F2 a, float* lo, float* hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(*lo), "=f"(*hi) : "l"(a.v));
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ float sum_of(F2 a) {
+  float lo, hi;
+  apart(a, &lo, &hi);
+  return lo + hi;
+}
+
 // ---- 8 elements of a row per thread.  VEC (rows start on 16-byte boundaries and cols is a multiple of 8):
 // eight neighbours, moved 16 bytes at a time, a chunk being whole or absent.  Otherwise (any alignment): eight
 // elements a multiple of 32 apart, so that the lanes of a warp touch neighbours and every group of 32 lies across
@@ -61,6 +95,25 @@ template <> struct Raw8<bf16> {
   __device__ __forceinline__ void put(const float (&v)[8]) {
     u = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
   }
+  __device__ __forceinline__ void get(F2 (&v)[4]) const {
+    v[0] = two(bf16_lo(u.x), bf16_hi(u.x)); v[1] = two(bf16_lo(u.y), bf16_hi(u.y));
+    v[2] = two(bf16_lo(u.z), bf16_hi(u.z)); v[3] = two(bf16_lo(u.w), bf16_hi(u.w));
+  }
+  __device__ __forceinline__ void put(const F2 (&v)[4]) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) apart(v[i], &f[2 * i], &f[2 * i + 1]);
+    put(f);
+  }
+  // bits of the largest magnitude, as a float's (NaN and Inf on top)
+  __device__ __forceinline__ uint32_t top() const {
+    const uint32_t k = 0x7FFF7FFFu;
+    uint32_t a, b;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(a) : "r"(u.x & k), "r"(u.y & k));
+    asm("max.u16x2 %0, %1, %2;" : "=r"(b) : "r"(u.z & k), "r"(u.w & k));
+    asm("max.u16x2 %0, %1, %2;" : "=r"(a) : "r"(a), "r"(b));
+    return max(a & 0xFFFF0000u, a << 16);
+  }
   __device__ __forceinline__ void load(const bf16* p) { u = *reinterpret_cast<const uint4*>(p); }
   __device__ __forceinline__ void store(bf16* p) const { *reinterpret_cast<uint4*>(p) = u; }
 };
@@ -72,6 +125,19 @@ template <> struct Raw8<float> {
   }
   __device__ __forceinline__ void put(const float (&v)[8]) {
     a = make_float4(v[0], v[1], v[2], v[3]); b = make_float4(v[4], v[5], v[6], v[7]);
+  }
+  __device__ __forceinline__ void get(F2 (&v)[4]) const {
+    v[0] = two(a.x, a.y); v[1] = two(a.z, a.w); v[2] = two(b.x, b.y); v[3] = two(b.z, b.w);
+  }
+  __device__ __forceinline__ void put(const F2 (&v)[4]) {
+    apart(v[0], &a.x, &a.y); apart(v[1], &a.z, &a.w); apart(v[2], &b.x, &b.y); apart(v[3], &b.z, &b.w);
+  }
+  __device__ __forceinline__ uint32_t top() const {
+    const float v[7] = {a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    float m = fabsf(a.x);
+#pragma unroll
+    for (int i = 0; i < 7; ++i) asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(m), "f"(fabsf(v[i])));
+    return __float_as_uint(m);
   }
   __device__ __forceinline__ void load(const float* p) {
     a = *reinterpret_cast<const float4*>(p); b = *reinterpret_cast<const float4*>(p + 4);
@@ -149,6 +215,24 @@ __device__ __forceinline__ void load_param(const ParamVec& w, const Place<VEC>& 
   }
 }
 
+// The same for 16-byte loads; the chunk has to lie within the vector.
+__device__ __forceinline__ void load_param(const ParamVec& w, int first, float none, F2 (&v)[4]) {
+  if (!w.p) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = two(none);
+  } else if (w.vec) {
+    if (w.is_bf16) { Raw8<bf16> r; r.load(static_cast<const bf16*>(w.p) + first); r.get(v); }
+    else { Raw8<float> r; r.load(static_cast<const float*>(w.p) + first); r.get(v); }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int j = first + 2 * i;
+      v[i] = w.is_bf16 ? two(to_float(static_cast<const bf16*>(w.p)[j]), to_float(static_cast<const bf16*>(w.p)[j + 1]))
+                       : two(static_cast<const float*>(w.p)[j], static_cast<const float*>(w.p)[j + 1]);
+    }
+  }
+}
+
 // Values as they stand in memory of type T.
 template <typename T>
 __device__ __forceinline__ void round_to(float (&v)[8]) {
@@ -178,39 +262,59 @@ __device__ __forceinline__ float act8_cut(float v) {
 }
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }   // NaN and Inf on top
 
-// The values at `p` (zeros past the row's end) into the checkpoint's row.  All 32 lanes call; `valid`: this
-// thread's chunk belongs to a row.  VEC: a group lies across an aligned quad of lanes.  The lane of the row's last
-// group also clears the scales' padding.
+// One chunk of values as they stand in memory (zeros past the row's end) into a checkpoint; the group lies across an
+// aligned quad of lanes.  All 32 lanes call; `codes` and `scales` point at the chunk's codes and the group's scale.
+// `keep`: the chunk belongs to a row and a group; `pad`: bytes of padding behind the row's last scale, for its lane.
+template <typename T>
+__device__ __forceinline__ void act8_put(uint8_t* codes, uint8_t* scales, const Raw8<T>& raw, bool first_of_group, int pad,
+                                         bool keep) {
+  uint32_t m = raw.top();
+  m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+  m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+  const uint32_t byte = act8_scale_byte(m);
+  const float inv = act8_inverse(byte);
+  F2 v[4];
+  raw.get(v);
+  uint32_t q[8];
+  const F2 inv2 = two(inv), magic = two(12582912.f);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float lo, hi;
+    apart(fma2(v[i], inv2, magic), &lo, &hi);
+    q[2 * i] = __float_as_uint(lo);
+    q[2 * i + 1] = __float_as_uint(hi);
+  }
+  if (byte == 249u) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float lo, hi;
+      apart(v[i], &lo, &hi);
+      q[2 * i] = act8_code(act8_cut(lo), inv);
+      q[2 * i + 1] = act8_code(act8_cut(hi), inv);
+    }
+  }
+  uint2 r;
+  r.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+  r.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
+  if (byte == 255u) r = make_uint2(0, 0);
+  if (!keep) return;
+  *reinterpret_cast<uint2*>(codes) = r;
+  if (first_of_group) {
+    *scales = static_cast<uint8_t>(byte);
+    for (int i = 1; i <= pad; ++i) scales[i] = 0;
+  }
+}
+
+// The same for values of any type at any place.
 template <bool VEC>
 __device__ __forceinline__ void act8_put(uint8_t* codes_row, uint8_t* scales_row, const Place<VEC>& p, int groups,
                                          const float (&v)[8], bool valid) {
   if constexpr (VEC) {
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[i]));
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-    const uint32_t byte = act8_scale_byte(m);
-    const float inv = act8_inverse(byte);
-    uint32_t q[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = act8_code(v[i], inv);
-    if (byte == 249u) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) q[i] = act8_code(act8_cut(v[i]), inv);
-    }
-    uint2 r;
-    r.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
-    r.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
-    if (byte == 255u) r = make_uint2(0, 0);
-    if (!valid || p.first >= groups * 32) return;
-    *reinterpret_cast<uint2*>(codes_row + p.first) = r;
-    if ((p.first & 31) == 0) {
-      const int g = p.first >> 5;
-      scales_row[g] = static_cast<uint8_t>(byte);
-      if (g == groups - 1)
-        for (int i = groups; i & 3; ++i) scales_row[i] = 0;
-    }
+    Raw8<float> raw;
+    raw.put(v);
+    const int g = p.first >> 5;
+    act8_put(codes_row + p.first, scales_row + g, raw, (p.first & 31) == 0, g == groups - 1 ? -groups & 3 : 0,
+             valid && g < groups);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -242,14 +346,22 @@ template <> struct RawAct8<true> {
       byte = scales_row[p.first >> 5];
     }
   }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
-    const float s = act8_scale(byte);
+  __device__ __forceinline__ void get(F2 (&v)[4]) const {
+    const F2 s = two(act8_scale(byte)), off = two(-8388736.f);
     const uint32_t a = q.x ^ 0x80808080u, b = q.y ^ 0x80808080u;   // code + 128 as an unsigned byte
+    // 2^23 + (code + 128) by its bits, minus the offset: exact
+    auto spread = [](uint32_t w, int i) { return __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7440 + i)); };
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {                                 // 2^23 + (code + 128) by its bits, minus the offset: exact
-      v[i] = (__uint_as_float(__byte_perm(a, 0x4B000000u, 0x7440 + i)) - 8388736.f) * s;
-      v[4 + i] = (__uint_as_float(__byte_perm(b, 0x4B000000u, 0x7440 + i)) - 8388736.f) * s;
+    for (int i = 0; i < 2; ++i) {
+      v[i] = mul2(add2(two(spread(a, 2 * i), spread(a, 2 * i + 1)), off), s);
+      v[2 + i] = mul2(add2(two(spread(b, 2 * i), spread(b, 2 * i + 1)), off), s);
     }
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    F2 u[4];
+    get(u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) apart(u[i], &v[2 * i], &v[2 * i + 1]);
   }
 };
 template <> struct RawAct8<false> {

@@ -27,6 +27,21 @@ __device__ __forceinline__ Place<VEC> split(const Flat& f, uint32_t i, uint32_t*
 }
 
 template <typename T, bool VEC>
+__device__ __forceinline__ void put_chunk(const Act8& ck, const Flat& f, uint32_t row, const Place<VEC>& p,
+                                          const Raw8<T>& raw, bool valid) {
+  uint8_t* codes = ck.codes + (size_t)row * f.groups * 32;
+  uint8_t* scales = ck.scales + (size_t)row * f.scale_pitch;
+  if constexpr (VEC) {
+    const int g = p.first >> 5;
+    act8_put(codes + p.first, scales + g, raw, (p.first & 31) == 0, g == f.groups - 1 ? -f.groups & 3 : 0, valid);
+  } else {
+    float v[8];
+    raw.get(v);
+    act8_put<VEC>(codes, scales, p, f.groups, v, valid);
+  }
+}
+
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads) store_kernel(const T* __restrict__ x, long long ldx, Act8 ck, Flat f) {
   const uint32_t first = blockIdx.x * (kThreads * kPer) + threadIdx.x;
   Raw8<T> raw[kPer];
@@ -40,12 +55,9 @@ __global__ void __launch_bounds__(kThreads) store_kernel(const T* __restrict__ x
   }
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
-    float v[8];
-    raw[k].get(v);
     const uint32_t i = first + k * kThreads;
     const Place<VEC> p = split<VEC>(f, i < f.n ? i : 0u, &row[k]);
-    act8_put<VEC>(ck.codes + (size_t)row[k] * f.groups * 32, ck.scales + (size_t)row[k] * f.scale_pitch, p, f.groups, v,
-                  i < f.n);
+    put_chunk<T, VEC>(ck, f, row[k], p, raw[k], i < f.n);
   }
 }
 
@@ -71,27 +83,77 @@ __global__ void __launch_bounds__(kThreads) load_kernel(Act8 ck, T* __restrict__
   }
 }
 
-// tanh form: z (1 + tanh u) / 2 = z * S(2u) with the logistic function S, u = sqrt(2/pi) (z + 0.044715 z^3)
-constexpr float kTwoU = 1.5957691216057308f;      // 2 sqrt(2/pi)
-__device__ __forceinline__ float logistic(float t, float) { return 1.f / (1.f + expf(-t)); }
-__device__ __forceinline__ float logistic(float t, bf16) { return __fdividef(1.f, 1.f + __expf(-t)); }
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// tanh form: z (1 + tanh u) / 2 = z S(2u) with the logistic function S and u = sqrt(2/pi) (z + 0.044715 z^3).
+// S is formed as 1 / (1 + 2^t), t = -2u log2(e): without the cancellation of 1 + tanh, two instructions of the
+// special function unit, off by a few units of 2^-23 wherever z S is not negligible.  z^2 is cut at 1000, where
+// 2^t has long run out of range, so that no product below overflows.
+constexpr float kT0 = -2.302208198144325f;            // -2 sqrt(2/pi) log2(e)
+constexpr float kT1 = kT0 * 0.044715f;
+constexpr float kU0 = 1.5957691216057308f;            // 2 sqrt(2/pi), of the derivative of 2u
+constexpr float kU1 = 3.f * 0.044715f * kU0;
+__device__ __forceinline__ F2 cut_square(F2 z) {
+  float a, b;
+  apart(mul2(z, z), &a, &b);
+  return two(fminf(a, 1000.f), fminf(b, 1000.f));
+}
+__device__ __forceinline__ F2 logistic_2u(F2 z, F2 z2) {
+  float a, b;
+  apart(mul2(z, fma2(z2, two(kT1), two(kT0))), &a, &b);
+  apart(add2(two(exp2_approx(a), exp2_approx(b)), two(1.f)), &a, &b);
+  return two(rcp_approx(a), rcp_approx(b));
+}
+
+// erf form: z Phi(z).  In bf16 Phi comes from Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26
+// (off by at most 1.5e-7, half of which reaches Phi), which shares its exponential with the density; in fp32 from
+// CUDA's normcdff.  `density` receives exp(-z^2 / 2) / sqrt(2 pi).
+template <typename T>
+__device__ __forceinline__ float normal_cdf(float z, float* density) {
+  const float e = exp2_approx(-0.7213475204444817f * z * z);      // exp(-z^2 / 2)
+  *density = e * 0.3989422804014327f;
+  if constexpr (sizeof(T) == 4) return normcdff(z);
+  const float t = rcp_approx(fmaf(0.3275911f * 0.7071067811865476f, fabsf(z), 1.f));
+  float q = fmaf(t, 1.061405429f, -1.453152027f);
+  q = fmaf(t, q, 1.421413741f);
+  q = fmaf(t, q, -0.284496736f);
+  q = fmaf(t, q, 0.254829592f);
+  q *= 0.5f * t * e;
+  return z >= 0.f ? 1.f - q : q;
+}
 
 template <typename T, int APPROX>
-__device__ __forceinline__ float gelu(float z) {
-  if constexpr (APPROX == kGeluTanh) return z * logistic(kTwoU * (z + 0.044715f * z * z * z), T());
-  else return z * normcdff(z);
-}
-template <typename T, int APPROX>
-__device__ __forceinline__ float gelu_slope(float z) {
+__device__ __forceinline__ void gelu(float& a, float& b) {
   if constexpr (APPROX == kGeluTanh) {
-    const float z2 = z * z;
-    const float s = logistic(kTwoU * (z + 0.044715f * z2 * z), T());
-    const float t = s * (1.f - s);
-    // far out t is zero while the other factors may overflow
-    return t == 0.f ? s : s + z * t * (kTwoU * (1.f + 3.f * 0.044715f * z2));
+    const F2 z = two(a, b);
+    apart(mul2(z, logistic_2u(z, cut_square(z))), &a, &b);
   } else {
-    const float e = expf(-0.5f * z * z) * 0.3989422804014327f;
-    return e == 0.f ? normcdff(z) : normcdff(z) + z * e;
+    float density;
+    a *= normal_cdf<T>(a, &density);
+    b *= normal_cdf<T>(b, &density);
+  }
+}
+// tanh form: S + z S (1 - S) (2u)'; erf form: Phi + z phi.
+template <typename T, int APPROX>
+__device__ __forceinline__ F2 gelu_slope(float a, float b) {
+  const F2 z = two(a, b);
+  if constexpr (APPROX == kGeluTanh) {
+    const F2 z2 = cut_square(z), s = logistic_2u(z, z2);
+    const F2 t = fma2(mul2(s, two(-1.f)), s, s);
+    return fma2(mul2(t, z), fma2(z2, two(kU1), two(kU0)), s);
+  } else {
+    float da, db;
+    const float pa = normal_cdf<T>(a, &da), pb = normal_cdf<T>(b, &db);
+    return fma2(z, two(da, db), two(pa, pb));
   }
 }
 
@@ -114,7 +176,6 @@ __global__ void __launch_bounds__(kThreads) gelu_forward_kernel(const T* __restr
     const uint32_t i = first + k * kThreads;
     const bool valid = i < f.n;
     const Place<VEC> p = split<VEC>(f, valid ? i : 0u, &row[k]);
-    const size_t code_row = (size_t)row[k] * f.groups * 32, scale_row = (size_t)row[k] * f.scale_pitch;
     float z[8], b[8];
     raw[k].get(z);
     if (bias.p) {
@@ -122,14 +183,20 @@ __global__ void __launch_bounds__(kThreads) gelu_forward_kernel(const T* __restr
 #pragma unroll
       for (int j = 0; j < 8; ++j) z[j] += b[j];
     }
-    if (ck_x.codes) act8_put<VEC>(ck_x.codes + code_row, ck_x.scales + scale_row, p, f.groups, z, valid);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) z[j] = gelu<T, APPROX>(z[j]);
-    if (valid) store_chunk<T, VEC>(y + row[k] * ldy, p, f.cols, z);
-    if (ck_y.codes) {
-      round_to<T>(z);                     // the checkpoint holds y as it is stored
-      act8_put<VEC>(ck_y.codes + code_row, ck_y.scales + scale_row, p, f.groups, z, valid);
+    if (ck_x.codes) {
+      Raw8<float> exact;                  // before any rounding
+      exact.put(z);
+      put_chunk<float, VEC>(ck_x, f, row[k], p, exact, valid);
     }
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) gelu<T, APPROX>(z[j], z[j + 1]);
+    raw[k].put(z);
+    if constexpr (VEC) {
+      if (valid && p.first < f.cols) raw[k].store(y + row[k] * ldy + p.first);
+    } else {
+      if (valid) store_chunk<T, VEC>(y + row[k] * ldy, p, f.cols, z);
+    }
+    if (ck_y.codes) put_chunk<T, VEC>(ck_y, f, row[k], p, raw[k], valid);     // y as it is stored
   }
 }
 
@@ -217,9 +284,10 @@ struct GeluBackward {
       for (int i = 0; i < 8; ++i) z[i] += b[i];
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      g[i] *= gelu_slope<T, APPROX>(z[i]);
-      acc[i] += g[i];
+    for (int i = 0; i < 8; i += 2) {
+      const F2 d = mul2(two(g[i], g[i + 1]), gelu_slope<T, APPROX>(z[i], z[i + 1]));
+      apart(d, &g[i], &g[i + 1]);
+      apart(add2(d, two(acc[i], acc[i + 1])), &acc[i], &acc[i + 1]);
     }
     store_chunk<T, VEC>(dx + r * lddx, p, cols, g);
   }
@@ -341,7 +409,8 @@ cudaError_t gelu_forward_d(Mat x, long long rows, long long cols, Param bias, in
              : gelu_forward_t<T, false, kGeluErf>(x, rows, cols, bias, y, ck_x, ck_y, st);
 }
 
-// Grid of a column kernel: about four blocks per SM in all, no block without rows.
+// Grid of a column kernel: sixteen blocks per SM, several times what is resident, so that the last ones to run leave
+// little of the GPU idle; but at least two loads ahead (2 * kAhead rows) for every thread as long as there are SMs to fill.
 struct ColumnGrid {
   int lanes_log2;
   unsigned x, y;
@@ -356,8 +425,10 @@ ColumnGrid column_grid(bool vec, long long rows, long long cols) {
   while (vec && g.lanes_log2 > 2 && (1LL << (g.lanes_log2 - 1)) >= g.chunks) --g.lanes_log2;
   const long long lanes = 1LL << g.lanes_log2, side = act8::kThreads / lanes;
   const long long x = (g.chunks + lanes - 1) / lanes;
-  long long y = (4LL * sm_count() + x - 1) / x;
-  const long long most = (rows + side - 1) / side;
+  const long long once = (2LL * sm_count() + x - 1) / x;
+  long long y = (16LL * sm_count() + x - 1) / x;
+  const long long full = (rows + side * 2 * act8::kAhead - 1) / (side * 2 * act8::kAhead), most = (rows + side - 1) / side;
+  if (y > full) y = full > once ? full : once;
   if (y > most) y = most;
   if (y < 1) y = 1;
   g.x = static_cast<unsigned>(x);

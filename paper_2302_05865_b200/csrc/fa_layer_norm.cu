@@ -22,19 +22,26 @@ struct Shape {
   int cols, groups, scale_pitch;
   int width;           // groups * 32
   int team;            // threads per row: a power of two up to 32 (not VEC: 32), or a multiple of 32
-  float n;             // cols: means are quotients, so a constant row has its own value as the mean
+  float n, inv;        // cols and its reciprocal
 };
 
 // Sums of N values over the team.  A team of several warps has a barrier of its own; `buf` has two sets of slots,
 // used in turn (`phase`), so that one barrier per call is enough.
 template <int N>
 __device__ __forceinline__ void team_sum(float (&v)[N], int team, float* buf, int* phase) {
-  const int top = team < 32 ? team : 32;
-  for (int o = top >> 1; o > 0; o >>= 1) {
+  if (team < 32) {
+    for (int o = team >> 1; o > 0; o >>= 1) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+    }
+    return;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
   }
-  if (team <= 32) return;
+  if (team == 32) return;
   constexpr int kWarps = kBlock / 32;
   float* b = buf + *phase * N * kWarps;
   *phase ^= 1;
@@ -44,12 +51,20 @@ __device__ __forceinline__ void team_sum(float (&v)[N], int team, float* buf, in
     for (int i = 0; i < N; ++i) b[warp * N + i] = v[i];
   }
   asm volatile("bar.sync %0, %1;" ::"r"(1 + mine), "r"(team) : "memory");
+  b += mine * warps * N;
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] = 0.f;
-  for (int w = mine * warps; w < (mine + 1) * warps; ++w) {
+#pragma unroll 4
+  for (int w = 0; w < warps; ++w) {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] += b[w * N + i];
   }
+}
+
+// Quotient of a sum and the number of columns, to the last bit but for rare ties; exact where it is a float.
+__device__ __forceinline__ float mean_of(float sum, const Shape& s) {
+  const float q = sum * s.inv;
+  return fmaf(fmaf(-q, s.n, sum), s.inv, q);
 }
 
 template <typename T>
@@ -65,8 +80,114 @@ struct Forward {
   Act8 ck_sum, ck_y;
 };
 
-template <typename T, bool VEC, int K>
+// Rows that 16-byte loads can address.  What bounds it is the number of instructions, so they work on two values
+// each where there is one that does, addresses are stepped, and a chunk is inside the row or not as a whole.
+template <typename T, int K>
+__global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1) forward_vec_kernel(Forward<T> a, Shape s) {
+  __shared__ float buf[2 * kBlock / 32];
+  int phase = 0;
+  const int teams = blockDim.x / s.team, t = threadIdx.x % s.team, mine = threadIdx.x / s.team;
+  const long long stride = (long long)gridDim.x * teams;
+  const int turns = static_cast<int>((s.rows + stride - 1) / stride);   // the same for every thread: all take part in the sums
+  long long r = (long long)blockIdx.x * teams + mine;
+  const int first = t * 8, apart_by = s.team * 8;               // chunk k starts at first + k * apart_by
+  const T* xp = a.x + r * a.ldx + first;
+  const T* up = a.residual ? a.residual + r * a.ldr + first : nullptr;
+  T* yp = a.y + r * a.ldy + first;
+  T* sp = a.sum_out ? a.sum_out + r * a.lds + first : nullptr;
+  long long code = r * s.width + first, scale = r * s.scale_pitch + (first >> 5);
+  const int pad = (first & 31) == 0 ? -s.groups & 3 : 0;
+  Raw8<T> x[K], u[K];
+  auto load = [&](bool live) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      x[k].zero();
+      u[k].zero();
+      if (live && first + k * apart_by < s.cols) {
+        x[k].load(xp + k * apart_by);
+        if (up) u[k].load(up + k * apart_by);
+      }
+    }
+  };
+  load(r < s.rows);
+  for (int i = 0; i < turns; ++i) {
+    const bool live = r < s.rows;
+    F2 v[K][4], part = two(0.f);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      x[k].get(v[k]);
+      if (up) {
+        F2 w[4];
+        u[k].get(w);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[k][j] = add2(v[k][j], w[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) part = add2(part, v[k][j]);
+    }
+    xp += stride * a.ldx;
+    if (up) up += stride * a.ldr;
+    load(r + stride < s.rows);
+    float sum[1] = {sum_of(part)};
+    team_sum(sum, s.team, buf, &phase);
+    const float mean = mean_of(sum[0], s);
+    const F2 minus_mean = two(-mean);
+    part = two(0.f);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (first + k * apart_by >= s.cols) continue;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const F2 d = add2(v[k][j], minus_mean);
+        part = fma2(d, d, part);
+      }
+    }
+    sum[0] = sum_of(part);
+    team_sum(sum, s.team, buf, &phase);
+    const float rstd = 1.f / sqrtf(mean_of(sum[0], s) + a.eps);
+    if (live && t == 0) {
+      if (a.mean) a.mean[r] = mean;
+      if (a.rstd) a.rstd[r] = rstd;
+    }
+    const F2 rstd2 = two(rstd);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int at = first + k * apart_by, g = at >> 5;
+      const bool in = at < s.cols, keep = live && g < s.groups;
+      Raw8<T> raw;
+      if (sp || a.ck_sum.codes) {
+        raw.put(v[k]);
+        if (live && in && sp) raw.store(sp + k * apart_by);
+        if (a.ck_sum.codes)               // the values as they are stored
+          act8_put(a.ck_sum.codes + code + k * apart_by, a.ck_sum.scales + scale + k * (apart_by >> 5), raw, (at & 31) == 0,
+                   g == s.groups - 1 ? pad : 0, keep);
+      }
+      raw.zero();
+      if (in) {
+        F2 w[4], b[4];
+        load_param(a.weight, at, 1.f, w);
+        load_param(a.bias, at, 0.f, b);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[k][j] = fma2(mul2(add2(v[k][j], minus_mean), rstd2), w[j], b[j]);
+        raw.put(v[k]);
+        if (live) raw.store(yp + k * apart_by);
+      }
+      if (a.ck_y.codes)
+        act8_put(a.ck_y.codes + code + k * apart_by, a.ck_y.scales + scale + k * (apart_by >> 5), raw, (at & 31) == 0,
+                 g == s.groups - 1 ? pad : 0, keep);
+    }
+    r += stride;
+    yp += stride * a.ldy;
+    if (sp) sp += stride * a.lds;
+    code += stride * s.width;
+    scale += stride * s.scale_pitch;
+  }
+}
+
+// Rows of any alignment, element by element.
+template <typename T, int K>
 __global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1) forward_kernel(Forward<T> a, Shape s) {
+  constexpr bool VEC = false;
   __shared__ float buf[2 * kBlock / 32];
   int phase = 0;
   const int teams = blockDim.x / s.team, t = threadIdx.x % s.team, mine = threadIdx.x / s.team;
@@ -82,9 +203,8 @@ __global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1)
       if (a.residual) u[k] = load_chunk<T, VEC>(a.residual + row * a.ldr, p, row < s.rows ? s.cols : 0);
     }
   };
-  if (VEC) load(r);
   for (long long i = 0; i < turns; ++i, r += stride) {
-    if (!VEC) load(r);                    // element by element: two rows at once would not fit the registers
+    load(r);                              // (two rows at once would not fit the registers)
     const bool live = r < s.rows;
     float v[K][8];
     float sum[1] = {0.f};
@@ -100,9 +220,8 @@ __global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1)
 #pragma unroll
       for (int j = 0; j < 8; ++j) sum[0] += v[k][j];
     }
-    if (VEC && i + 1 < turns) load(r + stride);
     team_sum(sum, s.team, buf, &phase);
-    const float mean = sum[0] / s.n;
+    const float mean = mean_of(sum[0], s);
     sum[0] = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -114,7 +233,7 @@ __global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1)
       }
     }
     team_sum(sum, s.team, buf, &phase);
-    const float rstd = 1.f / sqrtf(sum[0] / s.n + a.eps);
+    const float rstd = 1.f / sqrtf(mean_of(sum[0], s) + a.eps);
     if (live && t == 0) {
       if (a.mean) a.mean[r] = mean;
       if (a.rstd) a.rstd[r] = rstd;
@@ -170,7 +289,7 @@ __global__ void __launch_bounds__(kBlock) forward_long_kernel(Forward<T> a, Shap
       for (int j = 0; j < 8; ++j) sum[0] += v[j];
     }
     team_sum(sum, kBlock, buf, &phase);
-    const float mean = sum[0] / s.n;
+    const float mean = mean_of(sum[0], s);
     sum[0] = 0.f;
     for (int i = 0; i < turns; ++i) {
       const Place<VEC> p(threadIdx.x, kBlock, i);
@@ -183,7 +302,7 @@ __global__ void __launch_bounds__(kBlock) forward_long_kernel(Forward<T> a, Shap
       }
     }
     team_sum(sum, kBlock, buf, &phase);
-    const float rstd = 1.f / sqrtf(sum[0] / s.n + a.eps);
+    const float rstd = 1.f / sqrtf(mean_of(sum[0], s) + a.eps);
     if (threadIdx.x == 0) {
       if (a.mean) a.mean[r] = mean;
       if (a.rstd) a.rstd[r] = rstd;
@@ -242,10 +361,159 @@ struct Input<T, VEC, true> {
   __device__ __forceinline__ void get(float (&v)[8]) const { x.get(v); }
 };
 
-// Persistent: a team walks over rows, its share of the column sums stays in registers.
-template <typename T, bool VEC, int K, bool CK>
+// The block's column sums (thread t of a team: element j of chunk k) into its partial sums.  `dyn`: [teams - 1] of
+// the team's values, element j of chunk k of thread t at (k * 8 + j) * team + t: neighbouring threads, neighbouring words.
+template <bool VEC, int K>
+__device__ __forceinline__ void write_partials(float* out, float* dyn, const Shape& s, int teams, int t, int mine,
+                                               const float (&dw)[K][8], const float (&db)[K][8]) {
+  const int all = s.team * 8 * K;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    if (teams > 1) {
+      __syncthreads();
+      if (mine > 0) {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) dyn[(mine - 1) * all + (k * 8 + j) * s.team + t] = half ? db[k][j] : dw[k][j];
+      }
+      __syncthreads();
+    }
+    if (mine > 0) continue;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const Place<VEC> p(t, s.team, k);
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[j] = half ? db[k][j] : dw[k][j];
+        for (int q = 0; q < teams - 1; ++q) v[j] += dyn[q * all + (k * 8 + j) * s.team + t];
+      }
+      store_chunk<float, VEC>(out + half * s.width, p, s.width, v);
+    }
+  }
+}
+
+// Persistent: a team walks over rows, its share of the column sums stays in registers.  For rows that 16-byte loads
+// can address; two values per instruction as in the forward pass.
+template <typename T, int K, bool CK>
+__global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1) backward_vec_kernel(Backward<T> a, Shape s) {
+  extern __shared__ float dyn[];
+  __shared__ float buf[2 * 2 * kBlock / 32];
+  int phase = 0;
+  const int teams = blockDim.x / s.team, t = threadIdx.x % s.team, mine = threadIdx.x / s.team;
+  const long long stride = (long long)gridDim.x * teams;
+  const int turns = static_cast<int>((s.rows + stride - 1) / stride);
+  long long r = (long long)blockIdx.x * teams + mine;
+  const int first = t * 8, apart_by = s.team * 8;
+  const T* dyp = a.dy + r * a.lddy + first;
+  const T* xp = CK ? nullptr : a.x + r * a.ldx + first;
+  const uint8_t* codes = CK ? a.ck.codes + r * s.width + first : nullptr;
+  const uint8_t* scales = CK ? a.ck.scales + r * s.scale_pitch + (first >> 5) : nullptr;
+  const T* up = a.residual ? a.residual + r * a.ldr + first : nullptr;
+  T* dxp = a.dx + r * a.lddx + first;
+  F2 dw[K][4], db[K][4];
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) dw[k][j] = db[k][j] = two(0.f);
+  Raw8<T> in_dy[K], in_x[CK ? 1 : K], in_u[K];
+  RawAct8<true> in_q[CK ? K : 1];
+  float mean = 0.f, rstd = 0.f;
+  auto load = [&](long long row) {
+    const bool live = row < s.rows;
+    mean = live ? a.mean[row] : 0.f;
+    rstd = live ? a.rstd[row] : 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const bool in = live && first + k * apart_by < s.cols;
+      in_dy[k].zero();
+      if (in) in_dy[k].load(dyp + k * apart_by);
+      if constexpr (CK) {
+        if (in) {
+          in_q[k].q = *reinterpret_cast<const uint2*>(codes + k * apart_by);
+          in_q[k].byte = scales[k * (apart_by >> 5)];
+        }
+      } else {
+        if (in) in_x[k].load(xp + k * apart_by);
+      }
+    }
+  };
+  load(r);
+  for (int i = 0; i < turns; ++i) {
+    const bool live = r < s.rows;
+    const F2 rstd2 = two(rstd), minus_mean = two(-mean);
+    F2 g[K][4], h[K][4], sg = two(0.f), sgh = two(0.f);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (!live || first + k * apart_by >= s.cols) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) g[k][j] = h[k][j] = two(0.f);
+        continue;
+      }
+      if (up) in_u[k].load(up + k * apart_by);
+      F2 w[4], dy[4];
+      load_param(a.weight, first + k * apart_by, 1.f, w);
+      in_dy[k].get(dy);
+      if constexpr (CK) in_q[k].get(h[k]);
+      else in_x[k].get(h[k]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        h[k][j] = mul2(add2(h[k][j], minus_mean), rstd2);
+        g[k][j] = mul2(dy[j], w[j]);
+        sg = add2(sg, g[k][j]);
+        sgh = fma2(g[k][j], h[k][j], sgh);
+        dw[k][j] = fma2(dy[j], h[k][j], dw[k][j]);
+        db[k][j] = add2(db[k][j], dy[j]);
+      }
+    }
+    dyp += stride * a.lddy;
+    if constexpr (CK) {
+      codes += stride * s.width;
+      scales += stride * s.scale_pitch;
+    } else {
+      xp += stride * a.ldx;
+    }
+    if (up) up += stride * a.ldr;
+    load(r + stride);
+    float sum[2] = {sum_of(sg), sum_of(sgh)};
+    team_sum(sum, s.team, buf, &phase);
+    const F2 mg = two(-sum[0] * s.inv), mgh = two(-sum[1] * s.inv);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (!live || first + k * apart_by >= s.cols) continue;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) g[k][j] = mul2(fma2(h[k][j], mgh, add2(g[k][j], mg)), rstd2);
+      if (a.residual) {
+        F2 u[4];
+        in_u[k].get(u);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) g[k][j] = add2(g[k][j], u[j]);
+      }
+      Raw8<T> o;
+      o.put(g[k]);
+      o.store(dxp + k * apart_by);
+    }
+    r += stride;
+    dxp += stride * a.lddx;
+  }
+  if (!a.partials) return;
+  float fw[K][8], fb[K][8];
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      apart(dw[k][j], &fw[k][2 * j], &fw[k][2 * j + 1]);
+      apart(db[k][j], &fb[k][2 * j], &fb[k][2 * j + 1]);
+    }
+  write_partials<true, K>(a.partials + (size_t)blockIdx.x * 2 * s.width, dyn, s, teams, t, mine, fw, fb);
+}
+
+// Rows of any alignment, element by element.
+template <typename T, int K, bool CK>
 __global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1) backward_kernel(Backward<T> a, Shape s) {
-  extern __shared__ float dyn[];             // [teams - 1][width]: column sums of the block's other teams
+  constexpr bool VEC = false;
+  extern __shared__ float dyn[];
   __shared__ float buf[2 * 2 * kBlock / 32];
   int phase = 0;
   const int teams = blockDim.x / s.team, t = threadIdx.x % s.team, mine = threadIdx.x / s.team;
@@ -271,9 +539,8 @@ __global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1)
       in_x[k].load(a, s, row, p, live);
     }
   };
-  if (VEC) load(r);
   for (long long i = 0; i < turns; ++i, r += stride) {
-    if (!VEC) load(r);
+    load(r);
     const bool live = r < s.rows;
     const float row_rstd = rstd;
     Raw8<T> dyr[K];
@@ -298,9 +565,8 @@ __global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1)
         db[k][j] += dy[j];
       }
     }
-    if (VEC && i + 1 < turns) load(r + stride);
     team_sum(sum, s.team, buf, &phase);
-    const float mg = sum[0] / s.n, mgh = sum[1] / s.n;
+    const float mg = mean_of(sum[0], s), mgh = mean_of(sum[1], s);
     if (!live) continue;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -319,35 +585,7 @@ __global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1)
       store_chunk<T, VEC>(a.dx + r * a.lddx, p, s.cols, o);
     }
   }
-  if (!a.partials) return;
-  float* out = a.partials + (size_t)blockIdx.x * 2 * s.width;
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    // element j of chunk k of thread t sits at (k * 8 + j) * team + t: neighbouring threads, neighbouring words
-    const int pad = s.team * 8 * K;
-    if (teams > 1) {
-      __syncthreads();
-      if (mine > 0) {
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) dyn[(mine - 1) * pad + (k * 8 + j) * s.team + t] = half ? db[k][j] : dw[k][j];
-      }
-      __syncthreads();
-    }
-    if (mine > 0) continue;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const Place<VEC> p(t, s.team, k);
-      float v[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        v[j] = half ? db[k][j] : dw[k][j];
-        for (int q = 0; q < teams - 1; ++q) v[j] += dyn[q * pad + (k * 8 + j) * s.team + t];
-      }
-      store_chunk<float, VEC>(out + half * s.width, p, s.width, v);
-    }
-  }
+  if (a.partials) write_partials<VEC, K>(a.partials + (size_t)blockIdx.x * 2 * s.width, dyn, s, teams, t, mine, dw, db);
 }
 
 // Long rows, first step: mean(g) and mean(g h) of every row.
@@ -376,8 +614,8 @@ __global__ void __launch_bounds__(kBlock) backward_stats_kernel(Backward<T> a, S
     }
     team_sum(sum, kBlock, buf, &phase);
     if (threadIdx.x == 0) {
-      stats[2 * r] = sum[0] / s.n;
-      stats[2 * r + 1] = sum[1] / s.n;
+      stats[2 * r] = mean_of(sum[0], s);
+      stats[2 * r + 1] = mean_of(sum[1], s);
     }
   }
 }
@@ -444,6 +682,7 @@ ln::Shape ln_shape(long long rows, long long cols) {
   s.width = s.groups * 32;
   s.scale_pitch = static_cast<int>(act8_scale_pitch(cols));
   s.n = static_cast<float>(cols);
+  s.inv = 1.f / s.n;
   return s;
 }
 
@@ -480,9 +719,15 @@ cudaError_t ln_forward_t(const ln::Forward<T>& a, long long rows, long long cols
   const long long want = (rows + teams - 1) / teams, most = (long long)sm_count() * ln_resident(K, threads);
   const unsigned grid = static_cast<unsigned>(want < most ? want : most);
   auto go = [&](auto kernel) { kernel<<<grid, threads, 0, st>>>(a, s); };
-  if (K == 1) go(ln::forward_kernel<T, VEC, 1>);
-  else if (K == 2) go(ln::forward_kernel<T, VEC, 2>);
-  else go(ln::forward_kernel<T, VEC, 4>);
+  if constexpr (VEC) {
+    if (K == 1) go(ln::forward_vec_kernel<T, 1>);
+    else if (K == 2) go(ln::forward_vec_kernel<T, 2>);
+    else go(ln::forward_vec_kernel<T, 4>);
+  } else {
+    if (K == 1) go(ln::forward_kernel<T, 1>);
+    else if (K == 2) go(ln::forward_kernel<T, 2>);
+    else go(ln::forward_kernel<T, 4>);
+  }
   return cudaGetLastError();
 }
 
@@ -539,8 +784,14 @@ cudaError_t ln_backward_t(const ln::Backward<T>& a, const LnBackwardGrid& g, flo
     ln::backward_long_kernel<T, VEC, CK><<<grid, 256, 0, st>>>(a, g.s, row_stats);
   } else {
     const size_t smem = a.partials ? (size_t)(g.teams - 1) * g.s.team * 8 * g.K * sizeof(float) : 0;
-    if (g.K == 1) ln::backward_kernel<T, VEC, 1, CK><<<g.grid, g.threads, smem, st>>>(a, g.s);
-    else ln::backward_kernel<T, VEC, 2, CK><<<g.grid, g.threads, smem, st>>>(a, g.s);
+    auto go = [&](auto kernel) { kernel<<<g.grid, g.threads, smem, st>>>(a, g.s); };
+    if constexpr (VEC) {
+      if (g.K == 1) go(ln::backward_vec_kernel<T, 1, CK>);
+      else go(ln::backward_vec_kernel<T, 2, CK>);
+    } else {
+      if (g.K == 1) go(ln::backward_kernel<T, 1, CK>);
+      else go(ln::backward_kernel<T, 2, CK>);
+    }
   }
   return cudaGetLastError();
 }
