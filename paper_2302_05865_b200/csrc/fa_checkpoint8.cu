@@ -319,6 +319,7 @@ __global__ void __launch_bounds__(32 * kFinishWarps) finish_columns_kernel(const
                                                                            int sums, long long width, long long cols,
                                                                            void* out0, void* out1, int gbf16) {
   __shared__ float s[kFinishWarps][32];
+  cudaGridDependencySynchronize();         // launched while the partial sums are still being written
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = blockIdx.y;
   const long long col = (long long)blockIdx.x * 32 + lane;
   void* out = k ? out1 : out0;
@@ -344,8 +345,17 @@ __global__ void __launch_bounds__(32 * kFinishWarps) finish_columns_kernel(const
 cudaError_t launch_finish_columns(const float* partials, int parts, int sums, long long width, long long cols,
                                   void* out0, void* out1, int gdtype, cudaStream_t st) {
   const dim3 grid((unsigned)((cols + 31) / 32), sums);
-  finish_columns_kernel<<<grid, 32 * kFinishWarps, 0, st>>>(partials, parts, sums, width, cols, out0, out1, gdtype == FA_BF16);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(32 * kFinishWarps);
+  cfg.stream = st;
+  cudaLaunchAttribute early{};
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &early;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, finish_columns_kernel, partials, parts, sums, width, cols, out0, out1,
+                            (int)(gdtype == FA_BF16));
 }
 
 // ---- host side

@@ -14,7 +14,9 @@ namespace fa {
 namespace ln {
 
 constexpr int kBlock = 512;             // most threads per row and block
-constexpr int kSmallBlock = 256;        // blocks of rows that take one chunk a thread: three of them per SM
+// One block per SM, as many threads as their registers allow: its teams' column sums are added in shared memory, so
+// that there are as few partial sums as SMs.
+template <typename T, int K> constexpr int kThreadsOf = K == 1 && sizeof(T) == 2 ? 768 : kBlock;
 constexpr int kMaxKForward = 4, kMaxKBackward = 2;
 
 struct Shape {
@@ -25,10 +27,23 @@ struct Shape {
   float n, inv;        // cols and its reciprocal
 };
 
-// Sums of N values over the team.  A team of several warps has a barrier of its own; `buf` has two sets of slots,
-// used in turn (`phase`), so that one barrier per call is enough.
+constexpr int kSlots = 16;              // warps of the widest team
+constexpr int kMaxTeams = 768 / 32;
+// Room for the sums of the warps of a team, two sets used in turn so that one barrier per call is enough; slots past
+// the team's warps stay zero, so that four are read at once.
 template <int N>
-__device__ __forceinline__ void team_sum(float (&v)[N], int team, float* buf, int* phase) {
+struct TeamSums {
+  alignas(16) float slot[2][N][kMaxTeams][kSlots];
+};
+template <int N>
+__device__ __forceinline__ void clear_sums(TeamSums<N>& buf) {
+  for (int i = threadIdx.x; i < 2 * N * kMaxTeams * kSlots; i += blockDim.x) (&buf.slot[0][0][0][0])[i] = 0.f;
+  __syncthreads();
+}
+
+// Sums of N values over the team.  A team of several warps has a barrier of its own.
+template <int N>
+__device__ __forceinline__ void team_sum(float (&v)[N], int team, TeamSums<N>& buf, int* phase) {
   if (team < 32) {
     for (int o = team >> 1; o > 0; o >>= 1) {
 #pragma unroll
@@ -42,23 +57,54 @@ __device__ __forceinline__ void team_sum(float (&v)[N], int team, float* buf, in
     for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
   }
   if (team == 32) return;
-  constexpr int kWarps = kBlock / 32;
-  float* b = buf + *phase * N * kWarps;
+  const int warps = team >> 5, warp = threadIdx.x >> 5, mine = warp / warps;
+  const int set = *phase;
   *phase ^= 1;
-  const int warp = threadIdx.x >> 5, warps = team >> 5, mine = warp / warps;
   if ((threadIdx.x & 31) == 0) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) b[warp * N + i] = v[i];
+    for (int i = 0; i < N; ++i) buf.slot[set][i][mine][warp - mine * warps] = v[i];
   }
   asm volatile("bar.sync %0, %1;" ::"r"(1 + mine), "r"(team) : "memory");
-  b += mine * warps * N;
 #pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = 0.f;
-#pragma unroll 4
-  for (int w = 0; w < warps; ++w) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] += b[w * N + i];
+  for (int i = 0; i < N; ++i) {
+    const float4* b = reinterpret_cast<const float4*>(buf.slot[set][i][mine]);
+    float4 q = b[0];
+    v[i] = (q.x + q.y) + (q.z + q.w);
+    if (warps > 4) {
+      q = b[1];
+      v[i] += (q.x + q.y) + (q.z + q.w);
+    }
+    if (warps > 8) {
+      q = b[2];
+      v[i] += (q.x + q.y) + (q.z + q.w);
+      q = b[3];
+      v[i] += (q.x + q.y) + (q.z + q.w);
+    }
   }
+}
+
+// A parameter vector as floats in shared memory, zeros past its end: element 4 i + j of a half, the first four
+// elements of every chunk in one half and the last four in the other, so that neighbouring lanes read neighbours.
+struct ParamCache {
+  float4* half[2];
+  __device__ __forceinline__ void get(int chunk, F2 (&v)[4]) const {
+    const float4 a = half[0][chunk], b = half[1][chunk];
+    v[0] = two(a.x, a.y); v[1] = two(a.z, a.w); v[2] = two(b.x, b.y); v[3] = two(b.z, b.w);
+  }
+};
+// Fills it; the caller synchronises.  `room`: 8 floats per chunk, 16-byte aligned.
+__device__ __forceinline__ ParamCache cache_param(float* room, const ParamVec& w, const Shape& s, float none) {
+  const int chunks = s.width / 8;
+  ParamCache c;
+  c.half[0] = reinterpret_cast<float4*>(room);
+  c.half[1] = c.half[0] + chunks;
+  for (int i = threadIdx.x; i < s.width; i += blockDim.x) {
+    float v = 0.f;
+    if (i < s.cols)
+      v = !w.p ? none : w.is_bf16 ? to_float(static_cast<const bf16*>(w.p)[i]) : static_cast<const float*>(w.p)[i];
+    room[((i & 4) ? chunks * 4 : 0) + (i >> 3) * 4 + (i & 3)] = v;
+  }
+  return c;
 }
 
 // Quotient of a sum and the number of columns, to the last bit but for rare ties; exact where it is a float.
@@ -83,8 +129,12 @@ struct Forward {
 // Rows that 16-byte loads can address.  What bounds it is the number of instructions, so they work on two values
 // each where there is one that does, addresses are stepped, and a chunk is inside the row or not as a whole.
 template <typename T, int K>
-__global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1) forward_vec_kernel(Forward<T> a, Shape s) {
-  __shared__ float buf[2 * kBlock / 32];
+__global__ void __launch_bounds__(kThreadsOf<T, K>, 1) forward_vec_kernel(Forward<T> a, Shape s) {
+  extern __shared__ float4 dyn4[];          // weight and bias
+  float* room = reinterpret_cast<float*>(dyn4);
+  const ParamCache weight = cache_param(room, a.weight, s, 1.f), bias = cache_param(room + s.width, a.bias, s, 0.f);
+  __shared__ TeamSums<1> buf;
+  clear_sums(buf);
   int phase = 0;
   const int teams = blockDim.x / s.team, t = threadIdx.x % s.team, mine = threadIdx.x / s.team;
   const long long stride = (long long)gridDim.x * teams;
@@ -144,7 +194,7 @@ __global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1)
     }
     sum[0] = sum_of(part);
     team_sum(sum, s.team, buf, &phase);
-    const float rstd = 1.f / sqrtf(mean_of(sum[0], s) + a.eps);
+    const float rstd = rsqrtf(mean_of(sum[0], s) + a.eps);
     if (live && t == 0) {
       if (a.mean) a.mean[r] = mean;
       if (a.rstd) a.rstd[r] = rstd;
@@ -165,8 +215,8 @@ __global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1)
       raw.zero();
       if (in) {
         F2 w[4], b[4];
-        load_param(a.weight, at, 1.f, w);
-        load_param(a.bias, at, 0.f, b);
+        weight.get(at >> 3, w);
+        bias.get(at >> 3, b);
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[k][j] = fma2(mul2(add2(v[k][j], minus_mean), rstd2), w[j], b[j]);
         raw.put(v[k]);
@@ -186,9 +236,10 @@ __global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1)
 
 // Rows of any alignment, element by element.
 template <typename T, int K>
-__global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1) forward_kernel(Forward<T> a, Shape s) {
+__global__ void __launch_bounds__(kThreadsOf<T, K>, 1) forward_kernel(Forward<T> a, Shape s) {
   constexpr bool VEC = false;
-  __shared__ float buf[2 * kBlock / 32];
+  __shared__ TeamSums<1> buf;
+  clear_sums(buf);
   int phase = 0;
   const int teams = blockDim.x / s.team, t = threadIdx.x % s.team, mine = threadIdx.x / s.team;
   const long long stride = (long long)gridDim.x * teams;
@@ -233,7 +284,7 @@ __global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1)
       }
     }
     team_sum(sum, s.team, buf, &phase);
-    const float rstd = 1.f / sqrtf(mean_of(sum[0], s) + a.eps);
+    const float rstd = rsqrtf(mean_of(sum[0], s) + a.eps);
     if (live && t == 0) {
       if (a.mean) a.mean[r] = mean;
       if (a.rstd) a.rstd[r] = rstd;
@@ -268,7 +319,8 @@ __global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1)
 // Rows of any length: one block per row, three reads.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kBlock) forward_long_kernel(Forward<T> a, Shape s) {
-  __shared__ float buf[2 * kBlock / 32];
+  __shared__ TeamSums<1> buf;
+  clear_sums(buf);
   int phase = 0;
   const int turns = (s.width / 8 + kBlock - 1) / kBlock;
   for (long long r = blockIdx.x; r < s.rows; r += gridDim.x) {
@@ -302,7 +354,7 @@ __global__ void __launch_bounds__(kBlock) forward_long_kernel(Forward<T> a, Shap
       }
     }
     team_sum(sum, kBlock, buf, &phase);
-    const float rstd = 1.f / sqrtf(mean_of(sum[0], s) + a.eps);
+    const float rstd = rsqrtf(mean_of(sum[0], s) + a.eps);
     if (threadIdx.x == 0) {
       if (a.mean) a.mean[r] = mean;
       if (a.rstd) a.rstd[r] = rstd;
@@ -397,9 +449,12 @@ __device__ __forceinline__ void write_partials(float* out, float* dyn, const Sha
 // Persistent: a team walks over rows, its share of the column sums stays in registers.  For rows that 16-byte loads
 // can address; two values per instruction as in the forward pass.
 template <typename T, int K, bool CK>
-__global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1) backward_vec_kernel(Backward<T> a, Shape s) {
-  extern __shared__ float dyn[];
-  __shared__ float buf[2 * 2 * kBlock / 32];
+__global__ void __launch_bounds__(kThreadsOf<T, K>, 1) backward_vec_kernel(Backward<T> a, Shape s) {
+  extern __shared__ float4 dyn4[];          // the weight; then the column sums of the block's other teams
+  float* dyn = reinterpret_cast<float*>(dyn4) + s.width;
+  const ParamCache weight = cache_param(reinterpret_cast<float*>(dyn4), a.weight, s, 1.f);
+  __shared__ TeamSums<2> buf;
+  clear_sums(buf);
   int phase = 0;
   const int teams = blockDim.x / s.team, t = threadIdx.x % s.team, mine = threadIdx.x / s.team;
   const long long stride = (long long)gridDim.x * teams;
@@ -417,7 +472,7 @@ __global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1)
   for (int k = 0; k < K; ++k)
 #pragma unroll
     for (int j = 0; j < 4; ++j) dw[k][j] = db[k][j] = two(0.f);
-  Raw8<T> in_dy[K], in_x[CK ? 1 : K], in_u[K];
+  Raw8<T> in_dy[K], in_x[CK ? 1 : K], in_u[K], next_u[K];
   RawAct8<true> in_q[CK ? K : 1];
   float mean = 0.f, rstd = 0.f;
   auto load = [&](long long row) {
@@ -437,11 +492,14 @@ __global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1)
       } else {
         if (in) in_x[k].load(xp + k * apart_by);
       }
+      if (in && up) next_u[k].load(up + k * apart_by);
     }
   };
   load(r);
   for (int i = 0; i < turns; ++i) {
     const bool live = r < s.rows;
+#pragma unroll
+    for (int k = 0; k < K; ++k) in_u[k] = next_u[k];
     const F2 rstd2 = two(rstd), minus_mean = two(-mean);
     F2 g[K][4], h[K][4], sg = two(0.f), sgh = two(0.f);
 #pragma unroll
@@ -451,9 +509,8 @@ __global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1)
         for (int j = 0; j < 4; ++j) g[k][j] = h[k][j] = two(0.f);
         continue;
       }
-      if (up) in_u[k].load(up + k * apart_by);
       F2 w[4], dy[4];
-      load_param(a.weight, first + k * apart_by, 1.f, w);
+      weight.get((first + k * apart_by) >> 3, w);
       in_dy[k].get(dy);
       if constexpr (CK) in_q[k].get(h[k]);
       else in_x[k].get(h[k]);
@@ -511,10 +568,11 @@ __global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1)
 
 // Rows of any alignment, element by element.
 template <typename T, int K, bool CK>
-__global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1) backward_kernel(Backward<T> a, Shape s) {
+__global__ void __launch_bounds__(kThreadsOf<T, K>, 1) backward_kernel(Backward<T> a, Shape s) {
   constexpr bool VEC = false;
   extern __shared__ float dyn[];
-  __shared__ float buf[2 * 2 * kBlock / 32];
+  __shared__ TeamSums<2> buf;
+  clear_sums(buf);
   int phase = 0;
   const int teams = blockDim.x / s.team, t = threadIdx.x % s.team, mine = threadIdx.x / s.team;
   const long long stride = (long long)gridDim.x * teams;
@@ -591,7 +649,8 @@ __global__ void __launch_bounds__(K == 1 ? kSmallBlock : kBlock, K == 1 ? 3 : 1)
 // Long rows, first step: mean(g) and mean(g h) of every row.
 template <typename T, bool VEC, bool CK>
 __global__ void __launch_bounds__(kBlock) backward_stats_kernel(Backward<T> a, Shape s, float* stats) {
-  __shared__ float buf[2 * 2 * kBlock / 32];
+  __shared__ TeamSums<2> buf;
+  clear_sums(buf);
   int phase = 0;
   const int turns = (s.width / 8 + kBlock - 1) / kBlock;
   for (long long r = blockIdx.x; r < s.rows; r += gridDim.x) {
@@ -686,12 +745,16 @@ ln::Shape ln_shape(long long rows, long long cols) {
   return s;
 }
 
-// Threads per row and chunks per thread; false: the row does not fit.  A thread for every chunk (8 values) of rows
-// of up to 256 chunks, since a row's time is mostly waiting; beyond, two and four chunks a thread.
-bool ln_team(ln::Shape* s, bool vec, int max_k, int* K) {
+// Threads per row and chunks (8 values) per thread; false: the row does not fit.  `few` and `many`: chunks per
+// thread of rows of up to 256 chunks, and of longer ones.
+bool ln_team(ln::Shape* s, bool vec, int few, int many, int max_k, int* K) {
   const int chunks = s->width / 8;
   if (chunks > ln::kBlock * max_k) return false;
-  *K = chunks <= ln::kSmallBlock ? 1 : chunks <= 2 * ln::kBlock ? 2 : 4;
+  *K = chunks <= 256 ? few : many;
+  while (*K * ln::kBlock < chunks) *K *= 2;
+  while (*K > 1 && chunks <= 32 * (*K / 2)) *K /= 2;
+  auto places = [&](int k) { return ((chunks + k - 1) / k + 31) / 32 * 32 * k; };
+  if (*K == 4 && places(3) < places(4) && 3 * ln::kBlock >= chunks) *K = 3;
   const int threads = (chunks + *K - 1) / *K;
   if (vec && threads <= 32) {
     int t = 4;
@@ -702,30 +765,42 @@ bool ln_team(ln::Shape* s, bool vec, int max_k, int* K) {
   }
   return true;
 }
-// Block size (whole teams) and blocks per SM.
-int ln_block(const ln::Shape& s) { return s.team <= ln::kSmallBlock ? ln::kSmallBlock / s.team * s.team : s.team; }
-int ln_resident(int K, int threads) { return (K == 1 ? 3 * ln::kSmallBlock : ln::kBlock) / threads; }
+// Block size: whole teams, a multiple of 32 threads, and no more teams than bring the rows to all SMs.
+int ln_block(const ln::Shape& s, int most) {
+  const int unit = s.team < 32 ? 32 : s.team, per_unit = unit / s.team;
+  const long long rows_per_sm = (s.rows + sm_count() - 1) / sm_count();
+  long long units = (rows_per_sm + per_unit - 1) / per_unit;
+  if (units > most / unit) units = most / unit;
+  return unit * static_cast<int>(units < 1 ? 1 : units);
+}
 
 template <typename T, bool VEC>
 cudaError_t ln_forward_t(const ln::Forward<T>& a, long long rows, long long cols, cudaStream_t st) {
   ln::Shape s = ln_shape(rows, cols);
   int K = 1;
-  if (!ln_team(&s, VEC, ln::kMaxKForward, &K)) {
+  const int few = VEC && sizeof(T) == 2 ? 4 : 1, many = VEC && sizeof(T) == 2 ? 4 : 2;
+  if (!ln_team(&s, VEC, few, many, ln::kMaxKForward, &K)) {
     const unsigned grid = static_cast<unsigned>(rows < (1 << 30) ? rows : 1 << 30);
     ln::forward_long_kernel<T, VEC><<<grid, ln::kBlock, 0, st>>>(a, s);
     return cudaGetLastError();
   }
-  const int threads = ln_block(s), teams = threads / s.team;
-  const long long want = (rows + teams - 1) / teams, most = (long long)sm_count() * ln_resident(K, threads);
+  const int threads = ln_block(s, K == 1 && sizeof(T) == 2 ? 768 : ln::kBlock), teams = threads / s.team;
+  const long long want = (rows + teams - 1) / teams, most = sm_count();
   const unsigned grid = static_cast<unsigned>(want < most ? want : most);
-  auto go = [&](auto kernel) { kernel<<<grid, threads, 0, st>>>(a, s); };
+  const size_t smem = VEC ? 2 * (size_t)s.width * sizeof(float) : 0;
+  auto go = [&](auto kernel) {
+    if (smem > 32 << 10) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    kernel<<<grid, threads, smem, st>>>(a, s);
+  };
   if constexpr (VEC) {
     if (K == 1) go(ln::forward_vec_kernel<T, 1>);
     else if (K == 2) go(ln::forward_vec_kernel<T, 2>);
+    else if (K == 3) go(ln::forward_vec_kernel<T, 3>);
     else go(ln::forward_vec_kernel<T, 4>);
   } else {
     if (K == 1) go(ln::forward_kernel<T, 1>);
     else if (K == 2) go(ln::forward_kernel<T, 2>);
+    else if (K == 3) go(ln::forward_kernel<T, 3>);
     else go(ln::forward_kernel<T, 4>);
   }
   return cudaGetLastError();
@@ -755,19 +830,19 @@ struct LnBackwardGrid {
   unsigned grid;
   bool is_long;
 };
-LnBackwardGrid ln_backward_grid(bool vec, long long rows, long long cols) {
+LnBackwardGrid ln_backward_grid(bool vec, int dtype, long long rows, long long cols) {
   LnBackwardGrid g{};
   g.s = ln_shape(rows, cols);
-  g.is_long = !ln_team(&g.s, vec, ln::kMaxKBackward, &g.K);
+  g.is_long = !ln_team(&g.s, vec, 1, 2, ln::kMaxKBackward, &g.K);
   long long want;
   if (g.is_long) {
     const long long tiles = (g.s.width + 255) / 256;
     g.threads = 256; g.teams = 8;
     want = (4LL * sm_count() + tiles - 1) / tiles;
   } else {
-    g.threads = ln_block(g.s);
+    g.threads = ln_block(g.s, g.K == 1 && dtype == FA_BF16 ? 768 : ln::kBlock);
     g.teams = g.threads / g.s.team;
-    want = (long long)sm_count() * ln_resident(g.K, g.threads);
+    want = sm_count();
   }
   const long long most = (rows + g.teams - 1) / g.teams;
   if (want > most) want = most;
@@ -783,8 +858,12 @@ cudaError_t ln_backward_t(const ln::Backward<T>& a, const LnBackwardGrid& g, flo
     const dim3 grid(g.grid, (g.s.width + 255) / 256);
     ln::backward_long_kernel<T, VEC, CK><<<grid, 256, 0, st>>>(a, g.s, row_stats);
   } else {
-    const size_t smem = a.partials ? (size_t)(g.teams - 1) * g.s.team * 8 * g.K * sizeof(float) : 0;
-    auto go = [&](auto kernel) { kernel<<<g.grid, g.threads, smem, st>>>(a, g.s); };
+    const size_t smem = (VEC ? (size_t)g.s.width * sizeof(float) : 0) +
+                        (a.partials ? (size_t)(g.teams - 1) * g.s.team * 8 * g.K * sizeof(float) : 0);
+    auto go = [&](auto kernel) {
+      if (smem > 32 << 10) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+      kernel<<<g.grid, g.threads, smem, st>>>(a, g.s);
+    };
     if constexpr (VEC) {
       if (g.K == 1) go(ln::backward_vec_kernel<T, 1, CK>);
       else go(ln::backward_vec_kernel<T, 2, CK>);
@@ -801,7 +880,7 @@ cudaError_t ln_backward_d(Mat dy, Mat x, const void* ck, long long rows, long lo
                           const float* mean, const float* rstd, Mat residual, Mat dx, void* dweight, void* dbias,
                           int gdtype, float* partials, float* row_stats, cudaStream_t st) {
   const bool vec = mat_vec<T>(dy, cols) && mat_vec<T>(x, cols) && mat_vec<T>(residual, cols) && mat_vec<T>(dx, cols);
-  const LnBackwardGrid g = ln_backward_grid(vec, rows, cols);
+  const LnBackwardGrid g = ln_backward_grid(vec, sizeof(T) == 2 ? FA_BF16 : FA_F32, rows, cols);
   const bool sums = dweight || dbias;
   if (rows > 0) {
     ln::Backward<T> a{};
@@ -826,8 +905,10 @@ cudaError_t ln_backward_d(Mat dy, Mat x, const void* ck, long long rows, long lo
 }  // namespace
 
 size_t layer_norm_partials_bytes(long long rows, long long cols) {
-  const LnBackwardGrid v = ln_backward_grid(true, rows, cols), e = ln_backward_grid(false, rows, cols);
-  return (size_t)(v.grid > e.grid ? v.grid : e.grid) * 2 * v.s.width * sizeof(float);   // alignment is known at the call
+  // type and alignment are known at the call: no grid has more blocks than there are SMs, or than 4 per SM for long rows
+  const LnBackwardGrid g = ln_backward_grid(true, FA_F32, rows, cols);
+  const long long most = g.is_long ? g.grid : sm_count();
+  return (size_t)(most < rows ? most : rows < 1 ? 1 : rows) * 2 * g.s.width * sizeof(float);
 }
 bool layer_norm_needs_row_stats(long long cols) { return act8_groups(cols) * 4 > ln::kBlock * ln::kMaxKBackward; }
 
