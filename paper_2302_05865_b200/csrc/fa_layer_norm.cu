@@ -16,7 +16,8 @@ namespace ln {
 constexpr int kBlock = 512;             // most threads per row and block
 // One block per SM, as many threads as their registers allow: its teams' column sums are added in shared memory, so
 // that there are as few partial sums as SMs.
-template <typename T, int K> constexpr int kThreadsOf = K == 1 && sizeof(T) == 2 ? 768 : kBlock;
+template <int K> constexpr int kForwardThreads = K == 1 ? 768 : kBlock;
+template <typename T, int K> constexpr int kBackwardThreads = K == 1 && sizeof(T) == 2 ? 768 : kBlock;
 constexpr int kMaxKForward = 4, kMaxKBackward = 2;
 
 struct Shape {
@@ -129,7 +130,7 @@ struct Forward {
 // Rows that 16-byte loads can address.  What bounds it is the number of instructions, so they work on two values
 // each where there is one that does, addresses are stepped, and a chunk is inside the row or not as a whole.
 template <typename T, int K>
-__global__ void __launch_bounds__(kThreadsOf<T, K>, 1) forward_vec_kernel(Forward<T> a, Shape s) {
+__global__ void __launch_bounds__(kForwardThreads<K>, 1) forward_vec_kernel(Forward<T> a, Shape s) {
   extern __shared__ float4 dyn4[];          // weight and bias
   float* room = reinterpret_cast<float*>(dyn4);
   const ParamCache weight = cache_param(room, a.weight, s, 1.f), bias = cache_param(room + s.width, a.bias, s, 0.f);
@@ -236,7 +237,7 @@ __global__ void __launch_bounds__(kThreadsOf<T, K>, 1) forward_vec_kernel(Forwar
 
 // Rows of any alignment, element by element.
 template <typename T, int K>
-__global__ void __launch_bounds__(kThreadsOf<T, K>, 1) forward_kernel(Forward<T> a, Shape s) {
+__global__ void __launch_bounds__(kForwardThreads<K>, 1) forward_kernel(Forward<T> a, Shape s) {
   constexpr bool VEC = false;
   __shared__ TeamSums<1> buf;
   clear_sums(buf);
@@ -449,7 +450,7 @@ __device__ __forceinline__ void write_partials(float* out, float* dyn, const Sha
 // Persistent: a team walks over rows, its share of the column sums stays in registers.  For rows that 16-byte loads
 // can address; two values per instruction as in the forward pass.
 template <typename T, int K, bool CK>
-__global__ void __launch_bounds__(kThreadsOf<T, K>, 1) backward_vec_kernel(Backward<T> a, Shape s) {
+__global__ void __launch_bounds__((kBackwardThreads<T, K>), 1) backward_vec_kernel(Backward<T> a, Shape s) {
   extern __shared__ float4 dyn4[];          // the weight; then the column sums of the block's other teams
   float* dyn = reinterpret_cast<float*>(dyn4) + s.width;
   const ParamCache weight = cache_param(reinterpret_cast<float*>(dyn4), a.weight, s, 1.f);
@@ -568,7 +569,7 @@ __global__ void __launch_bounds__(kThreadsOf<T, K>, 1) backward_vec_kernel(Backw
 
 // Rows of any alignment, element by element.
 template <typename T, int K, bool CK>
-__global__ void __launch_bounds__(kThreadsOf<T, K>, 1) backward_kernel(Backward<T> a, Shape s) {
+__global__ void __launch_bounds__((kBackwardThreads<T, K>), 1) backward_kernel(Backward<T> a, Shape s) {
   constexpr bool VEC = false;
   extern __shared__ float dyn[];
   __shared__ TeamSums<2> buf;
@@ -784,7 +785,7 @@ cudaError_t ln_forward_t(const ln::Forward<T>& a, long long rows, long long cols
     ln::forward_long_kernel<T, VEC><<<grid, ln::kBlock, 0, st>>>(a, s);
     return cudaGetLastError();
   }
-  const int threads = ln_block(s, K == 1 && sizeof(T) == 2 ? 768 : ln::kBlock), teams = threads / s.team;
+  const int threads = ln_block(s, K == 1 ? 768 : ln::kBlock), teams = threads / s.team;
   const long long want = (rows + teams - 1) / teams, most = sm_count();
   const unsigned grid = static_cast<unsigned>(want < most ? want : most);
   const size_t smem = VEC ? 2 * (size_t)s.width * sizeof(float) : 0;

@@ -68,6 +68,7 @@ struct Params {
   int tiles_i, tiles;            // tiles along the inputs, in all
   int splits;
   int ksteps;                    // steps in all: stages of tokens x terms
+  int run;                       // steps summed in the accumulator before they are added to the result in fp32
   void* dw;                      // splits == 1
   int gbf16;
   float* partials;               // splits > 1: [splits][split_stride]
@@ -285,22 +286,25 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
     if (rank == 0 && elect_one()) {
       uint32_t n = 0, nu = 0;
       bool ok = true;
-      for (int u = first_unit; u < units && ok; u += unit_step, ++nu) {
+      for (int u = first_unit; u < units && ok; u += unit_step) {
         const Unit w = unit_of<N, PAIR>(prm, u, rank);
-        const uint32_t acc = nu & 1, d = tmem_base + acc * N;
-        ok = mbar_wait(&bars->acc_empty[acc], ((nu >> 1) & 1) ^ 1);
-        for (int j = w.k0; j < w.k1 && ok; ++j, ++n) {
-          const int s = n % C::kStages;
-          ok = mbar_wait(&bars->full[s], (n / C::kStages) & 1);
-          if (!ok) break;
-          tc_fence_after();
-          const uint32_t a = smem_u32(stages + (size_t)s * C::kStage), b = a + kBytesA;
+        for (int j0 = w.k0; j0 < w.k1 && ok; j0 += prm.run, ++nu) {
+          const int j1 = min(j0 + prm.run, w.k1);
+          const uint32_t acc = nu & 1, d = tmem_base + acc * N;
+          ok = mbar_wait(&bars->acc_empty[acc], ((nu >> 1) & 1) ^ 1);
+          for (int j = j0; j < j1 && ok; ++j, ++n) {
+            const int s = n % C::kStages;
+            ok = mbar_wait(&bars->full[s], (n / C::kStages) & 1);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t a = smem_u32(stages + (size_t)s * C::kStage), b = a + kBytesA;
 #pragma unroll
-          for (int q = 0; q < kTokens / 16; ++q)        // 16 tokens are two groups of 8: 2048 bytes
-            umma<PAIR>(d, mn_desc(a + q * 2048), mn_desc(b + q * 2048), C::kIdesc, (j == w.k0 && q == 0) ? 0u : 1u);
-          umma_commit<PAIR>(&bars->empty[s]);
+            for (int q = 0; q < kTokens / 16; ++q)      // 16 tokens are two groups of 8: 2048 bytes
+              umma<PAIR>(d, mn_desc(a + q * 2048), mn_desc(b + q * 2048), C::kIdesc, (j == j0 && q == 0) ? 0u : 1u);
+            umma_commit<PAIR>(&bars->empty[s]);
+          }
+          if (ok) umma_commit<PAIR>(&bars->acc_full[acc]);
         }
-        if (ok) umma_commit<PAIR>(&bars->acc_full[acc]);
       }
       if (!ok) {                                        // products under way must end before the block may exit
         umma_commit<PAIR>(&bars->drained);
@@ -309,42 +313,55 @@ __global__ void __launch_bounds__(kThreads, 1) weight_grad_kernel(const __grid_c
     }
     __syncwarp();
   } else if (warp < 6) {
-    // ---------------- read-out: warp w reads the 32 accumulator rows of its quarter
+    // ---------------- read-out: warp w reads the 32 accumulator rows of its quarter.  The tensor cores cut the sums
+    // off rather than rounding them, an error that grows with the number of additions (1.8e-5 of the result after
+    // 32768 tokens), so a sum wanted in fp32 is formed in runs (4.5e-7): the first is stored, the others are added to
+    // it in L2.  Only this thread ever touches the element, one run after the other, so the order is fixed; an
+    // atomic addition is used because nothing has to wait for it (a load, add and store took 100 us of 590 for
+    // 16384 x 4096 x 4096).
     const int quarter = warp & 3;
     uint32_t nu = 0;
     bool ok = true;
-    for (int u = first_unit; u < units; u += unit_step, ++nu) {
+    for (int u = first_unit; u < units; u += unit_step) {
       const Unit w = unit_of<N, PAIR>(prm, u, rank);
-      const uint32_t acc = nu & 1;
-      ok = __all_sync(0xffffffffu, ok && mbar_wait(&bars->acc_full[acc], (nu >> 1) & 1));
-      tc_fence_after();
       const int i = w.i0 + quarter * 32 + lane;
-      float* part = prm.partials + (size_t)w.split * prm.split_stride;
-      for (int c = 0; c < N; c += 32) {
-        uint32_t v[32];
-        if (ok) {
-          tmem_ld32(tmem_base + (static_cast<uint32_t>(32 * quarter) << 16) + acc * N + c, v);
-          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-        } else {                                       // a wait ran out: the result shows it
+      float* sums = prm.splits > 1 ? prm.partials + (size_t)w.split * prm.split_stride : static_cast<float*>(prm.dw);
+      const bool to_bf16 = prm.splits == 1 && prm.gbf16;
+      for (int j0 = w.k0; j0 < w.k1; j0 += prm.run, ++nu) {
+        const uint32_t acc = nu & 1;
+        ok = __all_sync(0xffffffffu, ok && mbar_wait(&bars->acc_full[acc], (nu >> 1) & 1));
+        tc_fence_after();
+        for (int c = 0; c < N; c += 32) {
+          uint32_t v[32];
+          if (ok) {
+            tmem_ld32(tmem_base + (static_cast<uint32_t>(32 * quarter) << 16) + acc * N + c, v);
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          } else {                                     // a wait ran out: the result shows it
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = 0x7FC00000u;
-        }
-        if (i < prm.ins) {
+            for (int j = 0; j < 32; ++j) v[j] = 0x7FC00000u;
+          }
+          const int left = prm.outs - (w.o0 + c);      // outputs from here on
+          if (i >= prm.ins || left <= 0) continue;
+          const size_t at = (size_t)(w.o0 + c) * prm.ins + i;
+          if (j0 > w.k0) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            const int o = w.o0 + c + j;
-            if (o >= prm.outs) break;
-            const size_t at = (size_t)o * prm.ins + i;
-            const float f = __uint_as_float(v[j]);
-            if (prm.splits > 1) part[at] = f;
-            else if (prm.gbf16) static_cast<bf16*>(prm.dw)[at] = __float2bfloat16_rn(f);
-            else static_cast<float*>(prm.dw)[at] = f;
+            for (int j = 0; j < 32; ++j)
+              if (j < left) atomicAdd(sums + at + (size_t)j * prm.ins, __uint_as_float(v[j]));
+          } else if (to_bf16) {
+            bf16* out = static_cast<bf16*>(prm.dw) + at;
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (j < left) out[(size_t)j * prm.ins] = __float2bfloat16_rn(__uint_as_float(v[j]));
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (j < left) sums[at + (size_t)j * prm.ins] = __uint_as_float(v[j]);
           }
         }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_first<PAIR>(&bars->acc_empty[acc]);
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) arrive_first<PAIR>(&bars->acc_empty[acc]);
     }
   } else if (warp < kScaleWarp) {
     // ---------------- converters: thread -> 8 codes of tokens t, t + 8, ..., t + 56 of the stage.  All eight
@@ -592,6 +609,7 @@ cudaError_t launch_linear_weight_grad(Mat dy, int dtype, long long rows, long lo
   prm.planes = p.planes;
   prm.tiles_i = p.tiles_i; prm.tiles = p.tiles; prm.splits = p.splits; prm.ksteps = p.ksteps;
   prm.dw = dweight; prm.gbf16 = gdtype == FA_BF16;
+  prm.run = gdtype == FA_BF16 ? p.ksteps : 32;      // (a bf16 result is rounded to 2^-9 anyway)
   prm.partials = reinterpret_cast<float*>(static_cast<char*>(scratch) + p.pack_bytes);
   prm.split_stride = p.split_stride;
   cudaError_t e = p.pair == 2  ? launch_product<256, 2>(map, map_codes, prm, st)

@@ -76,25 +76,29 @@ def _row_stride(t, name):
     return t.shape[-1] if ld is None else ld
 
 
-def _matrix(t, name, like=None):
-    """(pointer, row stride, rows, cols) of an activation; `like`: (rows, cols, dtype, device) it has to share."""
-    _code(t, name)
-    if t.dim() < 1 or t.shape[-1] < 1:
+def _matrix(t, name):
+    """(pointer, row stride, rows, cols, type code, device) of the activation that sets a call's shape."""
+    code = _code(t, name)
+    shape = t.shape
+    if not shape or shape[-1] < 1:
         raise ValueError(f"{name} must have a last dimension of at least one element")
-    cols = t.shape[-1]
-    rows = t.numel() // cols
-    if like is not None and (rows, cols, t.dtype) != like[:3]:
-        raise ValueError(f"{name} must have {like[0]} rows of {like[1]} elements of {like[2]}, got {rows} of {cols} of {t.dtype}")
+    cols = shape[-1]
     ld = cols if t.is_contiguous() else _row_stride(t, name)
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
-    if like is not None and t.device != like[3]:
-        raise ValueError(f"{name} is on {t.device}, the call runs on {like[3]}")
-    return t.data_ptr(), ld, rows, cols
+    return t.data_ptr(), ld, t.numel() // cols, cols, code, t.device
 
 
-def _opt_matrix(t, name, like):
-    return (None, 0) if t is None else _matrix(t, name, like)[:2]
+def _like(t, name, rows, cols, dtype, device):
+    """(pointer, row stride) of another activation of the same call."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.dtype != dtype or t.numel() != rows * cols or not t.dim() or t.shape[-1] != cols:
+        raise ValueError(f"{name} must have {rows} rows of {cols} elements of {dtype}, got {tuple(t.shape)} of {t.dtype}")
+    ld = cols if t.is_contiguous() else _row_stride(t, name)
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the call runs on {device}")
+    return t.data_ptr(), ld
 
 
 def _vector(t, numel, name, device, dtype=None):
@@ -109,20 +113,14 @@ def _vector(t, numel, name, device, dtype=None):
         raise ValueError(f"{name} must be contiguous")
     if t.numel() != numel:
         raise ValueError(f"{name} must have {numel} elements, got {t.numel()}")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, the call runs on {device}")
     return t.data_ptr()
 
 
-def _params(first, second, numel, names, device):
-    """Pointers and common type code of two optional parameter vectors."""
-    given = [t for t in (first, second) if t is not None]
-    ptrs = [None if t is None else _vector(t, numel, n, device) for t, n in zip((first, second), names)]
-    if len(given) == 2 and given[0].dtype != given[1].dtype:
-        raise ValueError(f"{names[0]} and {names[1]} must have the same dtype")
-    return ptrs[0], ptrs[1], _CODES[given[0].dtype] if given else FA_F32
+def _param(t, numel, name, device):
+    """(pointer, type code) of an optional parameter vector."""
+    return (None, FA_F32) if t is None else (_vector(t, numel, name, device), _CODES[t.dtype])
 
 
 def _buffer(t, nbytes, name, device):
@@ -144,31 +142,27 @@ def _opt_checkpoint(t, rows, cols, name, device):
     return None if t is None else _buffer(t, fa_checkpoint8_bytes(rows, cols), name, device)
 
 
-def _grads(first, second, shapes, names, device):
-    """Tensors for two parameter gradients (see the module's docstring for None and False)."""
-    given = [t for t in (first, second) if isinstance(t, torch.Tensor)]
-    for t, n in zip((first, second), names):
-        if t is not None and t is not False and not isinstance(t, torch.Tensor):
-            raise TypeError(f"{n} must be a torch tensor, None or False")
-    dtype = given[0].dtype if given else torch.float32
-    if len(given) == 2 and given[1].dtype != dtype:
-        raise ValueError(f"{names[0]} and {names[1]} must have the same dtype")
-    out, ptrs = [], []
-    for t, shape, n in zip((first, second), shapes, names):
-        if t is False:
-            out.append(None)
-            ptrs.append(None)
-            continue
-        if t is None:
-            t = torch.empty(shape, dtype=dtype, device=device)
-        numel = 1
-        for k in shape:
-            numel *= k
-        out.append(t)
-        ptrs.append(_vector(t, numel, n, device))
-    if dtype not in _CODES:
-        raise TypeError(f"{names[0]} and {names[1]} must be float32 or bfloat16, got {dtype}")
-    return out, ptrs, _CODES[dtype]
+def _grad(t, shape, numel, name, device, partner=None):
+    """(tensor or None, pointer) of a parameter gradient (see the module's docstring for None and False)."""
+    if t is False:
+        return None, None
+    if t is None:
+        like = partner if isinstance(partner, torch.Tensor) else None
+        t = torch.empty(shape, dtype=torch.float32 if like is None else like.dtype, device=device)
+        return t, t.data_ptr()
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor, None or False")
+    return t, _vector(t, numel, name, device)
+
+
+def _grad_code(first, second, names):
+    """Common type code of two gradients, either of which may be None."""
+    one = first if first is not None else second
+    if one is None:
+        return FA_F32
+    if first is not None and second is not None and first.dtype != second.dtype:
+        raise ValueError(f"{names} must have the same dtype")
+    return _CODES[one.dtype]
 
 
 def _on(device, stream):
@@ -180,8 +174,13 @@ def _on(device, stream):
     return torch.cuda.stream(stream)
 
 
-def _handle(device):
-    return torch.cuda.current_stream(device).cuda_stream
+# handle of the current stream (torch.cuda.current_stream(device).cuda_stream is a fifth of a small call's time)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _fresh(like):
+    """A dense tensor of the shape and type of `like`."""
+    return torch.empty_like(like, memory_format=torch.contiguous_format)
 
 
 def _workspace(ws, nbytes, device):
@@ -217,12 +216,13 @@ def new_checkpoint8(rows: int, cols: int, device) -> torch.Tensor:
 
 def fa_checkpoint8_store(x, ck=None, stream=None):
     """Checkpoint of the activations x; returns its buffer."""
-    xp, ldx, rows, cols = _matrix(x, "x")
-    dev = x.device
+    xp, ldx, rows, cols, code, dev = _matrix(x, "x")
     with _on(dev, stream):
-        ck = new_checkpoint8(rows, cols, dev) if ck is None else ck
-        cp = _opt_checkpoint(ck, rows, cols, "ck", dev)
-        _check(_lib.fa_checkpoint8_store(xp, ldx, _CODES[x.dtype], rows, cols, cp, _handle(dev)), "fa_checkpoint8_store")
+        nbytes = fa_checkpoint8_bytes(rows, cols)
+        if ck is None:
+            ck = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        _check(_lib.fa_checkpoint8_store(xp, ldx, code, rows, cols, _buffer(ck, nbytes, "ck", dev), _raw_stream(dev.index)),
+               "fa_checkpoint8_store")
     return ck
 
 
@@ -233,9 +233,11 @@ def fa_checkpoint8_load(ck, rows, cols, out=None, dtype=torch.bfloat16, stream=N
     dev = ck.device
     cp = _buffer(ck, fa_checkpoint8_bytes(rows, cols), "ck", dev)
     with _on(dev, stream):
-        out = torch.empty((rows, cols), dtype=dtype, device=dev) if out is None else out
-        op, ldo, _, _ = _matrix(out, "out", (rows, cols, out.dtype, dev))
-        _check(_lib.fa_checkpoint8_load(cp, _CODES[out.dtype], rows, cols, op, ldo, _handle(dev)), "fa_checkpoint8_load")
+        if out is None:
+            out = torch.empty((rows, cols), dtype=dtype, device=dev)
+        code = _code(out, "out")
+        op, ldo = _like(out, "out", rows, cols, out.dtype, dev)
+        _check(_lib.fa_checkpoint8_load(cp, code, rows, cols, op, ldo, _raw_stream(dev.index)), "fa_checkpoint8_load")
     return out
 
 
@@ -246,24 +248,32 @@ def fa_layer_norm_forward(x, weight=None, bias=None, eps=1e-5, residual=None, y=
     Without a residual s is x itself (sum_out None).  ck_sum / ck_y: buffers of new_checkpoint8() that
     receive the checkpoints of s and of y.
     """
-    xp, ldx, rows, cols = _matrix(x, "x")
-    dev = x.device
-    like = (rows, cols, x.dtype, dev)
-    rp, ldr = _opt_matrix(residual, "residual", like)
-    wp, bp, pcode = _params(weight, bias, cols, ("weight", "bias"), dev)
+    xp, ldx, rows, cols, code, dev = _matrix(x, "x")
+    dtype = x.dtype
+    rp, ldr = (None, 0) if residual is None else _like(residual, "residual", rows, cols, dtype, dev)
+    wp, pcode = _param(weight, cols, "weight", dev)
+    bp, bcode = _param(bias, cols, "bias", dev)
+    if wp is None:
+        pcode = bcode
+    elif bp is not None and bcode != pcode:
+        raise ValueError("weight and bias must have the same dtype")
     with _on(dev, stream):
-        y = torch.empty(x.shape, dtype=x.dtype, device=dev) if y is None else y
+        yp, ldy = _like(y, "y", rows, cols, dtype, dev) if y is not None else (None, cols)
+        if y is None:
+            y = _fresh(x)
+            yp = y.data_ptr()
         if sum_out is None and residual is not None:
-            sum_out = torch.empty(x.shape, dtype=x.dtype, device=dev)
-        mean = torch.empty(rows, dtype=torch.float32, device=dev) if mean is None else mean
-        rstd = torch.empty(rows, dtype=torch.float32, device=dev) if rstd is None else rstd
-        yp, ldy = _matrix(y, "y", like)[:2]
-        sp, lds = _opt_matrix(sum_out, "sum_out", like)
+            sum_out = _fresh(x)
+        sp, lds = (None, 0) if sum_out is None else _like(sum_out, "sum_out", rows, cols, dtype, dev)
+        if mean is None:
+            mean = torch.empty(rows, dtype=torch.float32, device=dev)
+        if rstd is None:
+            rstd = torch.empty(rows, dtype=torch.float32, device=dev)
         _check(_lib.fa_layer_norm_forward(
-            xp, ldx, rp, ldr, _CODES[x.dtype], rows, cols, wp, bp, pcode, eps, yp, ldy, sp, lds,
+            xp, ldx, rp, ldr, code, rows, cols, wp, bp, pcode, eps, yp, ldy, sp, lds,
             _vector(mean, rows, "mean", dev, torch.float32), _vector(rstd, rows, "rstd", dev, torch.float32),
             _opt_checkpoint(ck_sum, rows, cols, "ck_sum", dev), _opt_checkpoint(ck_y, rows, cols, "ck_y", dev),
-            _handle(dev)), "fa_layer_norm_forward")
+            _raw_stream(dev.index)), "fa_layer_norm_forward")
     return y, mean, rstd, x if sum_out is None else sum_out
 
 
@@ -277,39 +287,45 @@ def fa_layer_norm_backward(dy, weight, mean, rstd, x=None, ck=None, residual_gra
 
     residual_grad is added to dx: the gradient that reaches s past the norm.
     """
-    dyp, lddy, rows, cols = _matrix(dy, "dy")
-    dev = dy.device
-    like = (rows, cols, dy.dtype, dev)
+    dyp, lddy, rows, cols, code, dev = _matrix(dy, "dy")
+    dtype = dy.dtype
     if (x is None) == (ck is None):
         raise ValueError("exactly one of x and ck must be given")
-    xp, ldx = _opt_matrix(x, "x", like)
+    xp, ldx = (None, 0) if x is None else _like(x, "x", rows, cols, dtype, dev)
     cp = _opt_checkpoint(ck, rows, cols, "ck", dev)
-    rp, ldr = _opt_matrix(residual_grad, "residual_grad", like)
-    wp, _, pcode = _params(weight, None, cols, ("weight", ""), dev)
+    rp, ldr = (None, 0) if residual_grad is None else _like(residual_grad, "residual_grad", rows, cols, dtype, dev)
+    wp, pcode = _param(weight, cols, "weight", dev)
     mp, sp = _vector(mean, rows, "mean", dev, torch.float32), _vector(rstd, rows, "rstd", dev, torch.float32)
     with _on(dev, stream):
-        dx = torch.empty(dy.shape, dtype=dy.dtype, device=dev) if dx is None else dx
-        dxp, lddx = _matrix(dx, "dx", like)[:2]
-        (dweight, dbias), (dwp, dbp), gcode = _grads(dweight, dbias, ((cols,), (cols,)), ("dweight", "dbias"), dev)
+        if dx is None:
+            dx = _fresh(dy)
+            dxp, lddx = dx.data_ptr(), cols
+        else:
+            dxp, lddx = _like(dx, "dx", rows, cols, dtype, dev)
+        given = dbias
+        dbias, dbp = _grad(dbias, (cols,), cols, "dbias", dev, dweight)
+        dweight, dwp = _grad(dweight, (cols,), cols, "dweight", dev, given)
         ws, wsp, wsb = _workspace(ws, fa_layer_norm_backward_workspace_bytes(rows, cols), dev)
         _check(_lib.fa_layer_norm_backward(
-            dyp, lddy, xp, ldx, cp, _CODES[dy.dtype], rows, cols, wp, pcode, mp, sp, rp, ldr, dxp, lddx, dwp, dbp, gcode,
-            wsp, wsb, _handle(dev)), "fa_layer_norm_backward")
+            dyp, lddy, xp, ldx, cp, code, rows, cols, wp, pcode, mp, sp, rp, ldr, dxp, lddx, dwp, dbp,
+            _grad_code(dweight, dbias, "dweight and dbias"), wsp, wsb, _raw_stream(dev.index)), "fa_layer_norm_backward")
     return dx, dweight, dbias
 
 
 def fa_gelu_forward(x, bias=None, approximate="tanh", y=None, ck_x=None, ck_y=None, stream=None):
     """gelu(x + bias); ck_x / ck_y receive the checkpoints of x + bias and of the result."""
-    xp, ldx, rows, cols = _matrix(x, "x")
-    dev = x.device
+    xp, ldx, rows, cols, code, dev = _matrix(x, "x")
     form = _approximate(approximate)
-    bp, _, pcode = _params(bias, None, cols, ("bias", ""), dev)
+    bp, pcode = _param(bias, cols, "bias", dev)
     with _on(dev, stream):
-        y = torch.empty(x.shape, dtype=x.dtype, device=dev) if y is None else y
-        yp, ldy = _matrix(y, "y", (rows, cols, x.dtype, dev))[:2]
+        if y is None:
+            y = _fresh(x)
+            yp, ldy = y.data_ptr(), cols
+        else:
+            yp, ldy = _like(y, "y", rows, cols, x.dtype, dev)
         _check(_lib.fa_gelu_forward(
-            xp, ldx, _CODES[x.dtype], rows, cols, bp, pcode, form, yp, ldy, _opt_checkpoint(ck_x, rows, cols, "ck_x", dev),
-            _opt_checkpoint(ck_y, rows, cols, "ck_y", dev), _handle(dev)), "fa_gelu_forward")
+            xp, ldx, code, rows, cols, bp, pcode, form, yp, ldy, _opt_checkpoint(ck_x, rows, cols, "ck_x", dev),
+            _opt_checkpoint(ck_y, rows, cols, "ck_y", dev), _raw_stream(dev.index)), "fa_gelu_forward")
     return y
 
 
@@ -319,27 +335,29 @@ def fa_gelu_backward_workspace_bytes(rows: int, cols: int) -> int:
 
 def fa_gelu_backward(dy, x=None, bias=None, ck=None, approximate="tanh", dx=None, dbias=None, ws=None, stream=None):
     """(dx, dbias) of fa_gelu_forward from its x and bias, or from ck_x, which holds their sum."""
-    dyp, lddy, rows, cols = _matrix(dy, "dy")
-    dev = dy.device
-    like = (rows, cols, dy.dtype, dev)
+    dyp, lddy, rows, cols, code, dev = _matrix(dy, "dy")
+    dtype = dy.dtype
     form = _approximate(approximate)
     if (x is None) == (ck is None):
         raise ValueError("exactly one of x and ck must be given")
     if ck is not None and bias is not None:
         raise ValueError("a checkpoint holds the input with its bias: bias must be None with ck")
-    xp, ldx = _opt_matrix(x, "x", like)
+    xp, ldx = (None, 0) if x is None else _like(x, "x", rows, cols, dtype, dev)
     cp = _opt_checkpoint(ck, rows, cols, "ck", dev)
-    bp, _, pcode = _params(bias, None, cols, ("bias", ""), dev)
+    bp, pcode = _param(bias, cols, "bias", dev)
     with _on(dev, stream):
-        dx = torch.empty(dy.shape, dtype=dy.dtype, device=dev) if dx is None else dx
-        dxp, lddx = _matrix(dx, "dx", like)[:2]
-        (dbias, _), (dbp, _), gcode = _grads(dbias, False, ((cols,), ()), ("dbias", ""), dev)
+        if dx is None:
+            dx = _fresh(dy)
+            dxp, lddx = dx.data_ptr(), cols
+        else:
+            dxp, lddx = _like(dx, "dx", rows, cols, dtype, dev)
+        dbias, dbp = _grad(dbias, (cols,), cols, "dbias", dev)
         wsp, wsb = None, 0
         if dbias is not None:
             ws, wsp, wsb = _workspace(ws, fa_gelu_backward_workspace_bytes(rows, cols), dev)
         _check(_lib.fa_gelu_backward(
-            dyp, lddy, xp, ldx, bp, pcode, cp, _CODES[dy.dtype], rows, cols, form, dxp, lddx, dbp, gcode, wsp, wsb,
-            _handle(dev)), "fa_gelu_backward")
+            dyp, lddy, xp, ldx, bp, pcode, cp, code, rows, cols, form, dxp, lddx, dbp, _grad_code(dbias, None, "dbias"),
+            wsp, wsb, _raw_stream(dev.index)), "fa_gelu_backward")
     return dx, dbias
 
 
@@ -349,14 +367,16 @@ def fa_linear_weight_grad_workspace_bytes(rows: int, outs: int, ins: int, dtype)
 
 def fa_linear_weight_grad(dy, ck, ins, dweight=None, dbias=None, ws=None, stream=None):
     """(dweight, dbias) of a linear layer: dy^T X and the column sums of dy, X (rows x ins) as held by ck."""
-    dyp, lddy, rows, outs = _matrix(dy, "dy")
-    dev = dy.device
+    dyp, lddy, rows, outs, code, dev = _matrix(dy, "dy")
     cp = _buffer(ck, fa_checkpoint8_bytes(rows, ins), "ck", dev)
     if dweight is False:
         raise ValueError("dweight cannot be left out")
     with _on(dev, stream):
-        (dweight, dbias), (dwp, dbp), gcode = _grads(dweight, dbias, ((outs, ins), (outs,)), ("dweight", "dbias"), dev)
-        ws, wsp, wsb = _workspace(ws, fa_linear_weight_grad_workspace_bytes(rows, outs, ins, dy.dtype), dev)
-        _check(_lib.fa_linear_weight_grad(dyp, lddy, _CODES[dy.dtype], rows, outs, cp, ins, dwp, dbp, gcode, wsp, wsb,
-                                          _handle(dev)), "fa_linear_weight_grad")
+        given = dbias
+        dbias, dbp = _grad(dbias, (outs,), outs, "dbias", dev, dweight)
+        dweight, dwp = _grad(dweight, (outs, ins), outs * ins, "dweight", dev, given)
+        ws, wsp, wsb = _workspace(ws, _bytes_of("fa_linear_weight_grad_workspace_bytes", rows, outs, ins, code), dev)
+        _check(_lib.fa_linear_weight_grad(dyp, lddy, code, rows, outs, cp, ins, dwp, dbp,
+                                          _grad_code(dweight, dbias, "dweight and dbias"), wsp, wsb,
+                                          _raw_stream(dev.index)), "fa_linear_weight_grad")
     return dweight, dbias
