@@ -1,5 +1,5 @@
 // 8-bit activation checkpoints and the element-wise operators around them: store, load, GELU forward
-// (with checkpoints), and the column kernels: GELU backward (from a checkpoint) and column sums.
+// (with checkpoints), and GELU backward (from a checkpoint, with the bias gradient).
 #include "../../include/fa.h"
 #include "fa_columns.cuh"
 #include "fa_train.h"
@@ -293,24 +293,6 @@ struct GeluBackward {
   }
 };
 
-template <typename T, bool VEC>
-struct ColumnSum {
-  static constexpr bool kVec = VEC;
-  const T* x; long long ldx;
-  int cols;
-  struct In { Raw8<T> x; };
-  __device__ __forceinline__ void begin(const Place<VEC>&) {}
-  __device__ __forceinline__ void load(long long r, const Place<VEC>& p, In& in) const {
-    in.x = load_chunk<T, VEC>(x + r * ldx, p, cols);
-  }
-  __device__ __forceinline__ void row(long long, const Place<VEC>&, const In& in, float (&acc)[8]) const {
-    float v[8];
-    in.x.get(v);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] += v[i];
-  }
-};
-
 }  // namespace act8
 
 // A block adds 32 columns of one sum, a warp taking every kFinishWarps-th part; the warps' sums are added in order.
@@ -499,17 +481,6 @@ cudaError_t gelu_backward_d(const GeluBackwardArgs& a, int approx, cudaStream_t 
   const bool vec = mat_vec<T>(a.dy, a.cols) && mat_vec<T>(a.x, a.cols) && mat_vec<T>(a.dx, a.cols);
   return vec ? gelu_backward_v<T, true>(a, approx, st) : gelu_backward_v<T, false>(a, approx, st);
 }
-template <typename T>
-cudaError_t column_sum_d(Mat x, long long rows, long long cols, void* out, int gdtype, float* partials,
-                         cudaStream_t st) {
-  if (mat_vec<T>(x, cols)) {
-    act8::ColumnSum<T, true> op{row_of<T>(x, 0), x.ld, static_cast<int>(cols)};
-    return run_columns(op, rows, cols, out, gdtype, partials, st);
-  }
-  act8::ColumnSum<T, false> op{row_of<T>(x, 0), x.ld, static_cast<int>(cols)};
-  return run_columns(op, rows, cols, out, gdtype, partials, st);
-}
-
 }  // namespace
 
 cudaError_t launch_act8_store(Mat x, int dtype, long long rows, long long cols, void* ck, cudaStream_t st) {
@@ -532,10 +503,4 @@ cudaError_t launch_gelu_backward(Mat dy, Mat x, Param bias, const void* ck, int 
   const GeluBackwardArgs a{dy, x, bias, ck, rows, cols, dx, dbias, gdtype, partials};
   return dtype == FA_BF16 ? gelu_backward_d<bf16>(a, approx, st) : gelu_backward_d<float>(a, approx, st);
 }
-cudaError_t launch_column_sum(Mat x, int dtype, long long rows, long long cols, void* out, int gdtype, float* partials,
-                              cudaStream_t st) {
-  return dtype == FA_BF16 ? column_sum_d<bf16>(x, rows, cols, out, gdtype, partials, st)
-                          : column_sum_d<float>(x, rows, cols, out, gdtype, partials, st);
-}
-
 }  // namespace fa

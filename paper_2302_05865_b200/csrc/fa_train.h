@@ -32,10 +32,6 @@ size_t column_partials_bytes(long long rows, long long cols);
 cudaError_t launch_gelu_backward(Mat dy, Mat x, Param bias, const void* ck, int dtype, long long rows, long long cols,
                                  int approx, Mat dx, void* dbias, int gdtype, float* partials, cudaStream_t st);
 
-// out = column sums of x
-cudaError_t launch_column_sum(Mat x, int dtype, long long rows, long long cols, void* out, int gdtype, float* partials,
-                              cudaStream_t st);
-
 cudaError_t launch_layer_norm_forward(Mat x, Mat residual, int dtype, long long rows, long long cols, Param weight,
                                       Param bias, float eps, Mat y, Mat sum_out, float* mean, float* rstd, void* ck_sum,
                                       void* ck_y, cudaStream_t st);
@@ -49,7 +45,7 @@ cudaError_t launch_layer_norm_backward(Mat dy, Mat x, const void* ck, int dtype,
                                        cudaStream_t st);
 
 cudaError_t launch_linear_weight_grad(Mat dy, int dtype, long long rows, long long outs, long long ins, const void* ck,
-                                      void* dweight, int gdtype, void* scratch, cudaStream_t st);
+                                      void* dweight, void* dbias, int gdtype, void* scratch, cudaStream_t st);
 size_t linear_weight_grad_scratch_bytes(long long rows, long long outs, long long ins, int dtype);
 
 }  // namespace fa

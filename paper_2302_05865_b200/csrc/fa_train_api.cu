@@ -39,12 +39,6 @@ size_t layer_norm_ws(long long rows, long long cols, size_t* stats_at) {
   if (stats_at) *stats_at = partials;
   return partials + (layer_norm_needs_row_stats(cols) ? ws_round((size_t)rows * 2 * sizeof(float)) : 0);
 }
-size_t weight_grad_ws(long long rows, long long outs, long long ins, int dtype, size_t* scratch_at) {
-  const size_t partials = ws_round(column_partials_bytes(rows, outs));
-  if (scratch_at) *scratch_at = partials;
-  return partials + ws_round(linear_weight_grad_scratch_bytes(rows, outs, ins, dtype));
-}
-
 }  // namespace
 }  // namespace fa
 
@@ -164,7 +158,7 @@ int fa_layer_norm_backward(const void* dy, long long lddy, const void* x, long l
 
 int fa_linear_weight_grad_workspace_bytes(long long rows, long long outs, long long ins, int dtype, size_t* bytes) {
   if (!bytes || !fa::type_ok(dtype) || !fa::product_ok(rows, outs, ins)) return FA_ERR_ARG;
-  *bytes = fa::weight_grad_ws(rows, outs, ins, dtype, nullptr);
+  *bytes = fa::ws_round(fa::linear_weight_grad_scratch_bytes(rows, outs, ins, dtype));
   return FA_OK;
 }
 
@@ -177,14 +171,9 @@ int fa_linear_weight_grad(const void* dy, long long lddy, int dtype, long long r
   if (!fa::at(dy, fa::size_of(dtype)) || !fa::at(ck, 16) || !fa::at(dweight, fa::size_of(gdtype)) ||
       !fa::at(dbias, fa::size_of(gdtype)) || !fa::at(ws, 16))
     return FA_ERR_ALIGN;
-  size_t scratch_at = 0;
-  if (ws_bytes < fa::weight_grad_ws(rows, outs, ins, dtype, &scratch_at)) return FA_ERR_WORKSPACE;
-  const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = fa::launch_linear_weight_grad({dy, lddy}, dtype, rows, outs, ins, ck, dweight, gdtype,
-                                                static_cast<char*>(ws) + scratch_at, st);
-  if (e == cudaSuccess && dbias)
-    e = fa::launch_column_sum({dy, lddy}, dtype, rows, outs, dbias, gdtype, static_cast<float*>(ws), st);
-  return fa::cuda_code(e);
+  if (ws_bytes < fa::linear_weight_grad_scratch_bytes(rows, outs, ins, dtype)) return FA_ERR_WORKSPACE;
+  return fa::cuda_code(fa::launch_linear_weight_grad({dy, lddy}, dtype, rows, outs, ins, ck, dweight, dbias, gdtype, ws,
+                                                     static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"
