@@ -68,10 +68,7 @@ __device__ __forceinline__ float sum_of(F2 a) {
   return lo + hi;
 }
 
-// ---- 8 elements of a row per thread.  VEC (rows start on 16-byte boundaries and cols is a multiple of 8):
-// eight neighbours, moved 16 bytes at a time, a chunk being whole or absent.  Otherwise (any alignment): eight
-// elements a multiple of 32 apart, so that the lanes of a warp touch neighbours and every group of 32 lies across
-// one warp; moved one by one.
+// ---- chunks: 8 neighbouring elements of a row per thread, neighbouring lanes holding neighbouring chunks
 __device__ __forceinline__ float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -114,6 +111,9 @@ template <> struct Raw8<bf16> {
     asm("max.u16x2 %0, %1, %2;" : "=r"(a) : "r"(a), "r"(b));
     return max(a & 0xFFFF0000u, a << 16);
   }
+  template <int N>
+  __device__ __forceinline__ void from_words(const uint32_t (&w)[N]) { u = make_uint4(w[0], w[1], w[2], w[3]); }
+  __device__ __forceinline__ void to_words(uint32_t (&w)[4]) const { w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w; }
   __device__ __forceinline__ void load(const bf16* p) { u = *reinterpret_cast<const uint4*>(p); }
   __device__ __forceinline__ void store(bf16* p) const { *reinterpret_cast<uint4*>(p) = u; }
 };
@@ -139,6 +139,15 @@ template <> struct Raw8<float> {
     for (int i = 0; i < 7; ++i) asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(m), "f"(fabsf(v[i])));
     return __float_as_uint(m);
   }
+  template <int N>
+  __device__ __forceinline__ void from_words(const uint32_t (&w)[N]) {
+    a = make_float4(__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3]));
+    b = make_float4(__uint_as_float(w[4]), __uint_as_float(w[5]), __uint_as_float(w[6]), __uint_as_float(w[7]));
+  }
+  __device__ __forceinline__ void to_words(uint32_t (&w)[8]) const {
+    w[0] = __float_as_uint(a.x); w[1] = __float_as_uint(a.y); w[2] = __float_as_uint(a.z); w[3] = __float_as_uint(a.w);
+    w[4] = __float_as_uint(b.x); w[5] = __float_as_uint(b.y); w[6] = __float_as_uint(b.z); w[7] = __float_as_uint(b.w);
+  }
   __device__ __forceinline__ void load(const float* p) {
     a = *reinterpret_cast<const float4*>(p); b = *reinterpret_cast<const float4*>(p + 4);
   }
@@ -147,43 +156,111 @@ template <> struct Raw8<float> {
   }
 };
 
-template <bool VEC>
-struct Place {
-  int first, step;
-  // chunk k of thread t when `width` threads (not VEC: a multiple of 32) share a row
-  __device__ __forceinline__ Place(int t, int width, int k)
-      : first(VEC ? (t + k * width) * 8 : k * width * 8 + t), step(VEC ? 1 : width) {}
-  __device__ __forceinline__ int at(int j) const { return first + j * step; }
-};
+// The first `valid` elements one by one, zeros behind them.
+template <typename T>
+__device__ __forceinline__ Raw8<T> load_some(const T* p, int valid) {
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = j < valid ? to_float(p[j]) : 0.f;
+  Raw8<T> r;
+  r.put(v);        // exact: the values have T's precision
+  return r;
+}
 
-// The elements, zeros past the row's end.
+// Words w[s / 4] onwards of a window, s in bytes: what lies s bytes into it.  s is a multiple of the element size and
+// below 16; OUT + 4 words (OUT for s = 0) are read.
+template <int OUT, bool HALVES>
+__device__ __forceinline__ void shift_window(uint32_t (&w)[OUT + 4], uint32_t s) {
+#pragma unroll
+  for (int i = 0; i < OUT + 2; ++i) w[i] = (s & 8) ? w[i + 2] : w[i];
+#pragma unroll
+  for (int i = 0; i < OUT + 1; ++i) w[i] = (s & 4) ? w[i + 1] : w[i];
+  if (HALVES) {
+#pragma unroll
+    for (int i = 0; i < OUT; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (s & 2) * 8);
+  }
+}
+
+// Elements first .. first + 7 of a row of `cols`, zeros past its end.  VEC: rows start on 16-byte boundaries and cols
+// is a multiple of 8, so a chunk is one aligned load (fp32: two), or lies outside.  Otherwise the chunk is cut out
+// of the aligned 16-byte blocks it lies in, where all of these are inside the row, and read one by one at its ends.
+// (All chunks read one by one, even by neighbouring lanes, took two to four times as long.)
 template <typename T, bool VEC>
-__device__ __forceinline__ Raw8<T> load_chunk(const T* row, const Place<VEC>& p, int cols) {
+__device__ __forceinline__ Raw8<T> load_chunk(const T* row, int first, int cols) {
   Raw8<T> r;
   if constexpr (VEC) {
-    if (p.first < cols) r.load(row + p.first);
+    if (first < cols) r.load(row + first);
     else r.zero();
   } else {
-    float v[8];
+    constexpr int kOut = 8 * sizeof(T) / 4, kPer = 16 / sizeof(T);       // words of a chunk, elements of a block
+    const uint32_t s = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row + first)) & 15u;
+    const int before = static_cast<int>(s / sizeof(T));                  // elements of the first block in front of the chunk
+    if (first >= before && first - before + 8 + kPer <= cols) {
+      const uint4* p = reinterpret_cast<const uint4*>(row + first - before);
+      uint32_t w[kOut + 4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = p.at(j) < cols ? to_float(row[p.at(j)]) : 0.f;
-    r.put(v);      // exact: the values have T's precision
+      for (int i = 0; i < kOut / 4 + 1; ++i) {
+        const uint4 b = p[i];
+        w[4 * i] = b.x; w[4 * i + 1] = b.y; w[4 * i + 2] = b.z; w[4 * i + 3] = b.w;
+      }
+      shift_window<kOut, sizeof(T) == 2>(w, s);
+      r.from_words(w);
+    } else {
+      r = load_some(row + first, cols - first);
+    }
   }
   return r;
 }
 
+// The reverse.  All 32 lanes call (not VEC: neighbours complete each other's blocks); `live`: there is something to
+// store; `prev` / `next`: the lane below / above holds the chunk in front / behind, of the same row and live too.
 template <typename T, bool VEC>
-__device__ __forceinline__ void store_chunk(T* row, const Place<VEC>& p, int cols, const float (&v)[8]) {
+__device__ __forceinline__ void store_chunk(T* row, int first, int cols, const Raw8<T>& r, bool live, bool prev, bool next) {
   if constexpr (VEC) {
-    if (p.first < cols) {
-      Raw8<T> r;
-      r.put(v);
-      r.store(row + p.first);
-    }
+    if (live && first < cols) r.store(row + first);
   } else {
+    constexpr int kOut = 8 * sizeof(T) / 4, kPer = 16 / sizeof(T);
+    uint32_t w[kOut + 4];
+    uint32_t own[kOut];
+    r.to_words(own);
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (p.at(j) < cols) row[p.at(j)] = from_float<T>(v[j]);
+    for (int i = 0; i < 4; ++i) w[i] = __shfl_up_sync(0xffffffffu, own[kOut - 4 + i], 1);
+#pragma unroll
+    for (int i = 0; i < kOut; ++i) w[4 + i] = own[i];
+    T* p = row + first;
+    const int valid = cols - first;
+    if (!live || valid <= 0) return;
+    const uint32_t s = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) & 15u;
+    const int before = static_cast<int>(s / sizeof(T));
+    float v[8];
+    r.get(v);
+    if (valid < 8) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < valid) p[j] = from_float<T>(v[j]);
+      return;
+    }
+    if (s == 0) {
+      r.store(p);
+      return;
+    }
+    // the blocks that end in this chunk; the first of them begins in the chunk in front
+    shift_window<kOut, sizeof(T) == 2>(w, 16 - s);
+    uint4* block = reinterpret_cast<uint4*>(p - before);
+    if (prev) {
+      block[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kPer; ++j)
+        if (j < kPer - before) p[j] = from_float<T>(v[j]);
+    }
+    if constexpr (sizeof(T) == 4) block[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    // its last elements belong to a block of the chunk behind, if that one is whole
+    if (!(next && valid >= 16)) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j >= 8 - before) p[j] = from_float<T>(v[j]);
+    }
   }
 }
 
@@ -191,54 +268,20 @@ __device__ __forceinline__ void store_chunk(T* row, const Place<VEC>& p, int col
 struct ParamVec {
   const void* p;       // null: the constant `none`
   int is_bf16;
-  int vec;             // 16-byte aligned and a multiple of 8 long
+  int vec;             // starts on a 16-byte boundary
 };
-template <bool VEC>
-__device__ __forceinline__ void load_param(const ParamVec& w, const Place<VEC>& p, int cols, float none, float (&v)[8]) {
-  if (!w.p) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = none;
+__device__ __forceinline__ void load_param(const ParamVec& w, int first, int cols, float none, float (&v)[8]) {
+  if (w.p && w.vec && first + 8 <= cols) {
+    if (w.is_bf16) { Raw8<bf16> r; r.load(static_cast<const bf16*>(w.p) + first); r.get(v); }
+    else { Raw8<float> r; r.load(static_cast<const float*>(w.p) + first); r.get(v); }
     return;
-  }
-  if constexpr (VEC) {
-    if (w.vec && p.first < cols) {
-      if (w.is_bf16) { Raw8<bf16> r; r.load(static_cast<const bf16*>(w.p) + p.first); r.get(v); }
-      else { Raw8<float> r; r.load(static_cast<const float*>(w.p) + p.first); r.get(v); }
-      return;
-    }
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
+    const int at = first + j;
     v[j] = none;
-    if (p.at(j) < cols)
-      v[j] = w.is_bf16 ? to_float(static_cast<const bf16*>(w.p)[p.at(j)]) : static_cast<const float*>(w.p)[p.at(j)];
-  }
-}
-
-// The same for 16-byte loads; the chunk has to lie within the vector.
-__device__ __forceinline__ void load_param(const ParamVec& w, int first, float none, F2 (&v)[4]) {
-  if (!w.p) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = two(none);
-  } else if (w.vec) {
-    if (w.is_bf16) { Raw8<bf16> r; r.load(static_cast<const bf16*>(w.p) + first); r.get(v); }
-    else { Raw8<float> r; r.load(static_cast<const float*>(w.p) + first); r.get(v); }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int j = first + 2 * i;
-      v[i] = w.is_bf16 ? two(to_float(static_cast<const bf16*>(w.p)[j]), to_float(static_cast<const bf16*>(w.p)[j + 1]))
-                       : two(static_cast<const float*>(w.p)[j], static_cast<const float*>(w.p)[j + 1]);
-    }
-  }
-}
-
-// Values as they stand in memory of type T.
-template <typename T>
-__device__ __forceinline__ void round_to(float (&v)[8]) {
-  if constexpr (sizeof(T) == 2) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = to_float(from_float<T>(v[i]));
+    if (w.p && at < cols)
+      v[j] = w.is_bf16 ? to_float(static_cast<const bf16*>(w.p)[at]) : static_cast<const float*>(w.p)[at];
   }
 }
 
@@ -260,7 +303,6 @@ __device__ __forceinline__ float act8_cut(float v) {
   const float top = 63.f * 5.316911983139664e36f;     // 63 * 2^122
   return fminf(fmaxf(v, -top), top);
 }
-__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }   // NaN and Inf on top
 
 // One chunk of values as they stand in memory (zeros past the row's end) into a checkpoint; the group lies across an
 // aligned quad of lanes.  All 32 lanes call; `codes` and `scales` point at the chunk's codes and the group's scale.
@@ -305,45 +347,17 @@ __device__ __forceinline__ void act8_put(uint8_t* codes, uint8_t* scales, const 
   }
 }
 
-// The same for values of any type at any place.
-template <bool VEC>
-__device__ __forceinline__ void act8_put(uint8_t* codes_row, uint8_t* scales_row, const Place<VEC>& p, int groups,
-                                         const float (&v)[8], bool valid) {
-  if constexpr (VEC) {
-    Raw8<float> raw;
-    raw.put(v);
-    const int g = p.first >> 5;
-    act8_put(codes_row + p.first, scales_row + g, raw, (p.first & 31) == 0, g == groups - 1 ? -groups & 3 : 0,
-             valid && g < groups);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t byte = act8_scale_byte(__reduce_max_sync(0xffffffffu, magnitude(v[j])));
-      const uint32_t q = byte == 255u ? 0u : act8_code(byte == 249u ? act8_cut(v[j]) : v[j], act8_inverse(byte));
-      const int i = p.at(j), g = i >> 5;
-      if (!valid || g >= groups) continue;
-      codes_row[i] = static_cast<uint8_t>(q);
-      if ((i & 31) == 0) {
-        scales_row[g] = static_cast<uint8_t>(byte);
-        if (g == groups - 1)
-          for (int k = groups; k & 3; ++k) scales_row[k] = 0;
-      }
-    }
-  }
-}
-
 // ---- decode
-// Codes and scales as they lie in memory.
-template <bool VEC> struct RawAct8;
-template <> struct RawAct8<true> {
+// A chunk's codes and its group's scale as they lie in memory; `inside`: the chunk belongs to a group.
+struct RawAct8 {
   uint2 q;
   uint32_t byte;
-  __device__ __forceinline__ void load(const uint8_t* codes_row, const uint8_t* scales_row, const Place<true>& p, int groups) {
+  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scale, bool inside) {
     q = make_uint2(0, 0);
     byte = 127;
-    if (p.first < groups * 32) {
-      q = *reinterpret_cast<const uint2*>(codes_row + p.first);
-      byte = scales_row[p.first >> 5];
+    if (inside) {
+      q = *reinterpret_cast<const uint2*>(codes);
+      byte = *scale;
     }
   }
   __device__ __forceinline__ void get(F2 (&v)[4]) const {
@@ -364,21 +378,6 @@ template <> struct RawAct8<true> {
     for (int i = 0; i < 4; ++i) apart(u[i], &v[2 * i], &v[2 * i + 1]);
   }
 };
-template <> struct RawAct8<false> {
-  float v_[8];
-  __device__ __forceinline__ void load(const uint8_t* codes_row, const uint8_t* scales_row, const Place<false>& p, int groups) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int i = p.at(j);
-      v_[j] = i < groups * 32 ? (float)static_cast<int8_t>(codes_row[i]) * act8_scale(scales_row[i >> 5]) : 0.f;
-    }
-  }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = v_[j];
-  }
-};
-
 // ---- division by a number fixed per launch, for 0 <= n < 2^31
 struct FastDiv {
   uint32_t d, mul, shift;

@@ -10,76 +10,68 @@ namespace act8 {
 constexpr int kThreads = 256;
 constexpr int kPer = 4;              // chunks per thread, loaded before any is worked on
 
-// A launch covers the chunks 0 .. n-1 of its rows, `per_row` each (VEC: 4 a group; otherwise 32 for every 256
-// elements, one per lane); n < 2^31.
+// A launch covers the chunks 0 .. n-1 of its rows, `per_row` (4 a group) each; n < 2^31.
 struct Flat {
   uint32_t n;
   int cols, groups, scale_pitch;
   FastDiv per_row;
 };
-
-template <bool VEC>
-__device__ __forceinline__ Place<VEC> split(const Flat& f, uint32_t i, uint32_t* row) {
-  *row = f.per_row.div(i);
-  const int c = static_cast<int>(i - *row * f.per_row.d);
-  if constexpr (VEC) return Place<VEC>(c, 0, 0);
-  else return Place<VEC>(c & 31, 32, c >> 5);
-}
-
-template <typename T, bool VEC>
-__device__ __forceinline__ void put_chunk(const Act8& ck, const Flat& f, uint32_t row, const Place<VEC>& p,
-                                          const Raw8<T>& raw, bool valid) {
-  uint8_t* codes = ck.codes + (size_t)row * f.groups * 32;
-  uint8_t* scales = ck.scales + (size_t)row * f.scale_pitch;
-  if constexpr (VEC) {
-    const int g = p.first >> 5;
-    act8_put(codes + p.first, scales + g, raw, (p.first & 31) == 0, g == f.groups - 1 ? -f.groups & 3 : 0, valid);
-  } else {
-    float v[8];
-    raw.get(v);
-    act8_put<VEC>(codes, scales, p, f.groups, v, valid);
+// One of them: chunk c of a row.
+struct At {
+  uint32_t row;
+  int c;
+  bool valid;
+  __device__ __forceinline__ At(const Flat& f, uint32_t i) : valid(i < f.n) {
+    if (!valid) i = 0;
+    row = f.per_row.div(i);
+    c = static_cast<int>(i - row * f.per_row.d);
   }
+};
+
+template <typename T>
+__device__ __forceinline__ void put_chunk(const Act8& ck, const Flat& f, const At& at, const Raw8<T>& raw) {
+  const int g = at.c >> 2;
+  act8_put(ck.codes + (size_t)at.row * f.groups * 32 + (size_t)at.c * 8, ck.scales + (size_t)at.row * f.scale_pitch + g, raw,
+           (at.c & 3) == 0, g == f.groups - 1 ? -f.groups & 3 : 0, at.valid);
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store_flat(T* out, long long ld, const Flat& f, const At& at, const Raw8<T>& raw) {
+  const int lane = threadIdx.x & 31;
+  store_chunk<T, VEC>(out + at.row * ld, at.c * 8, f.cols, raw, at.valid, at.c > 0 && lane > 0,
+                      at.c + 1 < static_cast<int>(f.per_row.d) && lane < 31);
 }
 
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads) store_kernel(const T* __restrict__ x, long long ldx, Act8 ck, Flat f) {
   const uint32_t first = blockIdx.x * (kThreads * kPer) + threadIdx.x;
   Raw8<T> raw[kPer];
-  uint32_t row[kPer];
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
-    const uint32_t i = first + k * kThreads;
-    const Place<VEC> p = split<VEC>(f, i < f.n ? i : 0u, &row[k]);
-    if (i < f.n) raw[k] = load_chunk<T, VEC>(x + row[k] * ldx, p, f.cols);
-    else raw[k].zero();
+    const At at(f, first + k * kThreads);
+    raw[k].zero();
+    if (at.valid) raw[k] = load_chunk<T, VEC>(x + at.row * ldx, at.c * 8, f.cols);
   }
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const uint32_t i = first + k * kThreads;
-    const Place<VEC> p = split<VEC>(f, i < f.n ? i : 0u, &row[k]);
-    put_chunk<T, VEC>(ck, f, row[k], p, raw[k], i < f.n);
-  }
+  for (int k = 0; k < kPer; ++k) put_chunk(ck, f, At(f, first + k * kThreads), raw[k]);
 }
 
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads) load_kernel(Act8 ck, T* __restrict__ out, long long ldo, Flat f) {
   const uint32_t first = blockIdx.x * (kThreads * kPer) + threadIdx.x;
-  RawAct8<VEC> q[kPer];
-  uint32_t row[kPer];
+  RawAct8 q[kPer];
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
-    const uint32_t i = first + k * kThreads;
-    const Place<VEC> p = split<VEC>(f, i < f.n ? i : 0u, &row[k]);
-    if (i < f.n) q[k].load(ck.codes + (size_t)row[k] * f.groups * 32, ck.scales + (size_t)row[k] * f.scale_pitch, p, f.groups);
+    const At at(f, first + k * kThreads);
+    q[k].load(ck.codes + (size_t)at.row * f.groups * 32 + (size_t)at.c * 8,
+              ck.scales + (size_t)at.row * f.scale_pitch + (at.c >> 2), at.valid);
   }
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
-    const uint32_t i = first + k * kThreads;
-    if (i >= f.n) continue;
-    const Place<VEC> p = split<VEC>(f, i, &row[k]);
-    float v[8];
+    F2 v[4];
     q[k].get(v);
-    store_chunk<T, VEC>(out + row[k] * ldo, p, f.cols, v);
+    Raw8<T> raw;
+    raw.put(v);
+    store_flat<T, VEC>(out, ldo, f, At(f, first + k * kThreads), raw);
   }
 }
 
@@ -163,90 +155,76 @@ __global__ void __launch_bounds__(kThreads) gelu_forward_kernel(const T* __restr
                                                                 Flat f) {
   const uint32_t first = blockIdx.x * (kThreads * kPer) + threadIdx.x;
   Raw8<T> raw[kPer];
-  uint32_t row[kPer];
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
-    const uint32_t i = first + k * kThreads;
-    const Place<VEC> p = split<VEC>(f, i < f.n ? i : 0u, &row[k]);
-    if (i < f.n) raw[k] = load_chunk<T, VEC>(x + row[k] * ldx, p, f.cols);
-    else raw[k].zero();
+    const At at(f, first + k * kThreads);
+    raw[k].zero();
+    if (at.valid) raw[k] = load_chunk<T, VEC>(x + at.row * ldx, at.c * 8, f.cols);
   }
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
-    const uint32_t i = first + k * kThreads;
-    const bool valid = i < f.n;
-    const Place<VEC> p = split<VEC>(f, valid ? i : 0u, &row[k]);
+    const At at(f, first + k * kThreads);
     float z[8], b[8];
     raw[k].get(z);
     if (bias.p) {
-      load_param<VEC>(bias, p, f.cols, 0.f, b);
+      load_param(bias, at.c * 8, f.cols, 0.f, b);
 #pragma unroll
       for (int j = 0; j < 8; ++j) z[j] += b[j];
     }
     if (ck_x.codes) {
       Raw8<float> exact;                  // before any rounding
       exact.put(z);
-      put_chunk<float, VEC>(ck_x, f, row[k], p, exact, valid);
+      put_chunk(ck_x, f, at, exact);
     }
 #pragma unroll
     for (int j = 0; j < 8; j += 2) gelu<T, APPROX>(z[j], z[j + 1]);
     raw[k].put(z);
-    if constexpr (VEC) {
-      if (valid && p.first < f.cols) raw[k].store(y + row[k] * ldy + p.first);
-    } else {
-      if (valid) store_chunk<T, VEC>(y + row[k] * ldy, p, f.cols, z);
-    }
-    if (ck_y.codes) put_chunk<T, VEC>(ck_y, f, row[k], p, raw[k], valid);     // y as it is stored
+    store_flat<T, VEC>(y, ldy, f, at, raw[k]);
+    if (ck_y.codes) put_chunk(ck_y, f, at, raw[k]);          // y as it is stored (zeros past the row's end: gelu(0) = 0)
   }
 }
 
-// ---- column kernels: a thread owns 8 columns and walks over rows; its sums stay in registers.  A block has
-// 256 / lanes rows side by side, `lanes` (a power of two; not VEC: 32) chunks wide.  Rows are taken kAhead at a
-// time, loads first.
+// ---- column kernels: a thread owns the 8 columns of a chunk and walks over rows; its sums stay in registers.  A block
+// has 256 / lanes rows side by side, `lanes` (a power of two; not VEC: 32, a warp) chunks wide.  Rows are taken kAhead
+// at a time, loads first.
 constexpr int kAhead = 4;
 struct Columns {
   long long rows;
-  int chunks, lanes_log2;    // chunks of a row: VEC 4 a group, otherwise 32 for every 256 elements
-  int width;                 // of the partial sums
-  float* partials;           // [gridDim.y][width], or null
+  int chunks, lanes_log2;
+  float* partials;           // [gridDim.y][chunks * 8], or null
 };
 
 template <class Op>
 __global__ void __launch_bounds__(kThreads) column_kernel(Op op, Columns g) {
-  constexpr bool VEC = Op::kVec;
   const int lanes = 1 << g.lanes_log2, side = kThreads >> g.lanes_log2;
   const int rl = threadIdx.x >> g.lanes_log2, lane = threadIdx.x & (lanes - 1);
   const int c = blockIdx.x * lanes + lane;
-  const Place<VEC> p = VEC ? Place<VEC>(c, 0, 0) : Place<VEC>(lane, 32, blockIdx.x);
   float acc[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) acc[i] = 0.f;
-  if (c < g.chunks) {
-    op.begin(p);
-    const long long step = (long long)gridDim.y * side;
-    for (long long r = (long long)blockIdx.y * side + rl; r < g.rows; r += step * kAhead) {
-      typename Op::In in[kAhead];
+  op.begin(c);
+  const long long step = (long long)gridDim.y * side;
+  for (long long r = (long long)blockIdx.y * side + rl; r < g.rows; r += step * kAhead) {
+    typename Op::In in[kAhead];
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k)
-        if (r + k * step < g.rows) op.load(r + k * step, p, in[k]);
+    for (int k = 0; k < kAhead; ++k)
+      if (r + k * step < g.rows) op.load(r + k * step, c, in[k]);
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k)
-        if (r + k * step < g.rows) op.row(r + k * step, p, in[k], acc);
-    }
+    for (int k = 0; k < kAhead; ++k)
+      if (r + k * step < g.rows) op.row(r + k * step, c, lane, in[k], acc);
   }
   if (!g.partials) return;
   __shared__ float sums[kThreads * 9];       // 9 floats apart: the threads of a column group spread over the banks
 #pragma unroll
   for (int i = 0; i < 8; ++i) sums[threadIdx.x * 9 + i] = acc[i];
   __syncthreads();
-  float* out = g.partials + (size_t)blockIdx.y * g.width;
+  const int width = g.chunks * 8;
+  float* out = g.partials + (size_t)blockIdx.y * width;
   for (int j = threadIdx.x; j < lanes * 8; j += kThreads) {
-    // column j of the block: element j / lanes of lane j % lanes, or (VEC) element j % 8 of lane j / 8
-    const int l = VEC ? j >> 3 : j & (lanes - 1), e = VEC ? j & 7 : j >> g.lanes_log2;
     const int col = blockIdx.x * lanes * 8 + j;
-    if (col >= g.width) continue;
+    if (col >= width) continue;
     float s = 0.f;
-    for (int k = 0; k < side; ++k) s += sums[(k * lanes + l) * 9 + e];
+    for (int k = 0; k < side; ++k) s += sums[(k * lanes + (j >> 3)) * 9 + (j & 7)];
     out[col] = s;
   }
 }
@@ -263,21 +241,26 @@ struct GeluBackward {
   float b[8];
   struct In {
     Raw8<T> dy, x;
-    RawAct8<VEC> q;
+    RawAct8 q;
   };
-  __device__ __forceinline__ void begin(const Place<VEC>& p) {
-    if (!CK) load_param<VEC>(bias, p, cols, 0.f, b);
+  __device__ __forceinline__ void begin(int c) {
+    if (!CK) load_param(bias, c * 8, cols, 0.f, b);
   }
-  __device__ __forceinline__ void load(long long r, const Place<VEC>& p, In& in) const {
-    in.dy = load_chunk<T, VEC>(dy + r * lddy, p, cols);
-    if constexpr (CK) in.q.load(ck.codes + (size_t)r * groups * 32, ck.scales + (size_t)r * scale_pitch, p, groups);
-    else in.x = load_chunk<T, VEC>(x + r * ldx, p, cols);
+  __device__ __forceinline__ void load(long long r, int c, In& in) const {
+    in.dy = load_chunk<T, VEC>(dy + r * lddy, c * 8, cols);
+    if constexpr (CK)
+      in.q.load(ck.codes + (size_t)r * groups * 32 + (size_t)c * 8, ck.scales + (size_t)r * scale_pitch + (c >> 2),
+                c < groups * 4);
+    else in.x = load_chunk<T, VEC>(x + r * ldx, c * 8, cols);
   }
-  __device__ __forceinline__ void row(long long r, const Place<VEC>& p, const In& in, float (&acc)[8]) const {
+  __device__ __forceinline__ void row(long long r, int c, int lane, const In& in, float (&acc)[8]) const {
     float g[8], z[8];
     in.dy.get(g);
     if constexpr (CK) {
-      in.q.get(z);
+      F2 v[4];
+      in.q.get(v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) apart(v[i], &z[2 * i], &z[2 * i + 1]);
     } else {
       in.x.get(z);
 #pragma unroll
@@ -289,7 +272,9 @@ struct GeluBackward {
       apart(d, &g[i], &g[i + 1]);
       apart(add2(d, two(acc[i], acc[i + 1])), &acc[i], &acc[i + 1]);
     }
-    store_chunk<T, VEC>(dx + r * lddx, p, cols, g);
+    Raw8<T> o;
+    o.put(g);
+    store_chunk<T, VEC>(dx + r * lddx, c * 8, cols, o, true, c > 0 && lane > 0, lane < 31);
   }
 };
 
@@ -345,8 +330,8 @@ namespace {
 
 // One launch per piece of at most 2^30 chunks (or one row, which has fewer than 2^28).
 template <class Launch>
-cudaError_t for_flat(bool vec, long long rows, long long cols, Launch launch) {
-  const long long groups = act8_groups(cols), per_row = vec ? groups * 4 : (groups + 7) / 8 * 32;
+cudaError_t for_flat(long long rows, long long cols, Launch launch) {
+  const long long groups = act8_groups(cols), per_row = groups * 4;
   const long long piece = (1LL << 30) / per_row;
   for (long long r0 = 0; r0 < rows; r0 += piece) {
     const long long n = rows - r0 < piece ? rows - r0 : piece;
@@ -367,7 +352,7 @@ cudaError_t for_flat(bool vec, long long rows, long long cols, Launch launch) {
 template <typename T>
 cudaError_t store_t(Mat x, long long rows, long long cols, void* ck, cudaStream_t st) {
   const bool vec = mat_vec<T>(x, cols);
-  return for_flat(vec, rows, cols, [&](unsigned blocks, const act8::Flat& f, long long r0) {
+  return for_flat(rows, cols, [&](unsigned blocks, const act8::Flat& f, long long r0) {
     if (vec) act8::store_kernel<T, true><<<blocks, act8::kThreads, 0, st>>>(row_of<T>(x, r0), x.ld, act8_at(ck, rows, cols, r0), f);
     else act8::store_kernel<T, false><<<blocks, act8::kThreads, 0, st>>>(row_of<T>(x, r0), x.ld, act8_at(ck, rows, cols, r0), f);
   });
@@ -375,7 +360,7 @@ cudaError_t store_t(Mat x, long long rows, long long cols, void* ck, cudaStream_
 template <typename T>
 cudaError_t load_t(const void* ck, long long rows, long long cols, Mat out, cudaStream_t st) {
   const bool vec = mat_vec<T>(out, cols);
-  return for_flat(vec, rows, cols, [&](unsigned blocks, const act8::Flat& f, long long r0) {
+  return for_flat(rows, cols, [&](unsigned blocks, const act8::Flat& f, long long r0) {
     if (vec) act8::load_kernel<T, true><<<blocks, act8::kThreads, 0, st>>>(act8_at(ck, rows, cols, r0), row_of<T>(out, r0), out.ld, f);
     else act8::load_kernel<T, false><<<blocks, act8::kThreads, 0, st>>>(act8_at(ck, rows, cols, r0), row_of<T>(out, r0), out.ld, f);
   });
@@ -383,8 +368,8 @@ cudaError_t load_t(const void* ck, long long rows, long long cols, Mat out, cuda
 template <typename T, bool VEC, int APPROX>
 cudaError_t gelu_forward_t(Mat x, long long rows, long long cols, Param bias, Mat y, void* ck_x, void* ck_y,
                            cudaStream_t st) {
-  const ParamVec b = param_vec(bias, cols);
-  return for_flat(VEC, rows, cols, [&](unsigned blocks, const act8::Flat& f, long long r0) {
+  const ParamVec b = param_vec(bias);
+  return for_flat(rows, cols, [&](unsigned blocks, const act8::Flat& f, long long r0) {
     act8::gelu_forward_kernel<T, VEC, APPROX><<<blocks, act8::kThreads, 0, st>>>(
         row_of<T>(x, r0), x.ld, b, row_of<T>(y, r0), y.ld, act8_at(ck_x, rows, cols, r0),
         act8_at(ck_y, rows, cols, r0), f);
@@ -406,13 +391,12 @@ cudaError_t gelu_forward_d(Mat x, long long rows, long long cols, Param bias, in
 struct ColumnGrid {
   int lanes_log2;
   unsigned x, y;
-  long long chunks, width;
+  long long chunks;
 };
 ColumnGrid column_grid(bool vec, long long rows, long long cols) {
   ColumnGrid g{};
   const long long groups = act8_groups(cols);
-  g.width = groups * 32;
-  g.chunks = vec ? groups * 4 : (groups + 7) / 8 * 32;
+  g.chunks = groups * 4;
   g.lanes_log2 = 5;
   while (vec && g.lanes_log2 > 2 && (1LL << (g.lanes_log2 - 1)) >= g.chunks) --g.lanes_log2;
   const long long lanes = 1LL << g.lanes_log2, side = act8::kThreads / lanes;
@@ -436,7 +420,6 @@ cudaError_t run_columns(const Op& op, long long rows, long long cols, void* out,
     act8::Columns p{};
     p.rows = rows;
     p.chunks = static_cast<int>(g.chunks);
-    p.width = static_cast<int>(g.width);
     p.lanes_log2 = g.lanes_log2;
     p.partials = out ? partials : nullptr;
     act8::column_kernel<Op><<<dim3(g.x, g.y), act8::kThreads, 0, st>>>(op, p);
@@ -444,7 +427,7 @@ cudaError_t run_columns(const Op& op, long long rows, long long cols, void* out,
     if (e != cudaSuccess) return e;
   }
   if (!out) return cudaSuccess;
-  return launch_finish_columns(partials, rows > 0 ? (int)g.y : 0, 1, g.width, cols, out, nullptr, gdtype, st);
+  return launch_finish_columns(partials, rows > 0 ? (int)g.y : 0, 1, g.chunks * 8, cols, out, nullptr, gdtype, st);
 }
 
 struct GeluBackwardArgs {
@@ -462,7 +445,7 @@ cudaError_t gelu_backward_t(const GeluBackwardArgs& a, cudaStream_t st) {
   act8::GeluBackward<T, VEC, APPROX, CK> op{};
   op.dy = row_of<T>(a.dy, 0); op.lddy = a.dy.ld;
   op.x = row_of<T>(a.x, 0); op.ldx = a.x.ld;
-  op.bias = param_vec(a.bias, a.cols);
+  op.bias = param_vec(a.bias);
   op.ck = act8_at(a.ck, a.rows, a.cols, 0);
   op.cols = static_cast<int>(a.cols);
   op.groups = static_cast<int>(act8_groups(a.cols));
@@ -496,7 +479,7 @@ cudaError_t launch_gelu_forward(Mat x, int dtype, long long rows, long long cols
 }
 size_t column_partials_bytes(long long rows, long long cols) {
   const ColumnGrid v = column_grid(true, rows, cols), e = column_grid(false, rows, cols);   // known at the call
-  return (size_t)(v.y > e.y ? v.y : e.y) * v.width * sizeof(float);
+  return (size_t)(v.y > e.y ? v.y : e.y) * v.chunks * 8 * sizeof(float);
 }
 cudaError_t launch_gelu_backward(Mat dy, Mat x, Param bias, const void* ck, int dtype, long long rows, long long cols,
                                  int approx, Mat dx, void* dbias, int gdtype, float* partials, cudaStream_t st) {

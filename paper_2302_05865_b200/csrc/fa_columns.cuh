@@ -16,11 +16,11 @@ inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 
 template <typename T> inline bool mat_vec(const Mat& m, long long cols) {
   return !m.p || (aligned16(m.p) && cols % 8 == 0 && (m.ld * (long long)sizeof(T)) % 16 == 0);
 }
-inline ParamVec param_vec(const Param& w, long long cols) {
+inline ParamVec param_vec(const Param& w) {
   ParamVec v{};
   v.p = w.p;
   v.is_bf16 = w.dtype == FA_BF16;
-  v.vec = w.p && aligned16(w.p) && cols % 8 == 0;
+  v.vec = aligned16(w.p);
   return v;
 }
 inline Act8 act8_at(const void* ck, long long rows, long long cols, long long row) {

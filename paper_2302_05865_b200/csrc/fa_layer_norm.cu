@@ -127,37 +127,35 @@ struct Forward {
   Act8 ck_sum, ck_y;
 };
 
-// Rows that 16-byte loads can address.  What bounds it is the number of instructions, so they work on two values
-// each where there is one that does, addresses are stepped, and a chunk is inside the row or not as a whole.
-template <typename T, int K>
-__global__ void __launch_bounds__(kForwardThreads<K>, 1) forward_vec_kernel(Forward<T> a, Shape s) {
+// What bounds it next to memory is the number of instructions, so they work on two values each where there is one that
+// does, and addresses are stepped.
+template <typename T, bool VEC, int K>
+__global__ void __launch_bounds__(kForwardThreads<K>, 1) forward_kernel(Forward<T> a, Shape s) {
   extern __shared__ float4 dyn4[];          // weight and bias
   float* room = reinterpret_cast<float*>(dyn4);
   const ParamCache weight = cache_param(room, a.weight, s, 1.f), bias = cache_param(room + s.width, a.bias, s, 0.f);
   __shared__ TeamSums<1> buf;
   clear_sums(buf);
   int phase = 0;
-  const int teams = blockDim.x / s.team, t = threadIdx.x % s.team, mine = threadIdx.x / s.team;
+  const int teams = blockDim.x / s.team, t = threadIdx.x % s.team, mine = threadIdx.x / s.team, lane = threadIdx.x & 31;
+  const bool prev = lane > 0 && t > 0, next = lane < 31 && t + 1 < s.team;      // neighbours of the same row
   const long long stride = (long long)gridDim.x * teams;
   const int turns = static_cast<int>((s.rows + stride - 1) / stride);   // the same for every thread: all take part in the sums
   long long r = (long long)blockIdx.x * teams + mine;
   const int first = t * 8, apart_by = s.team * 8;               // chunk k starts at first + k * apart_by
-  const T* xp = a.x + r * a.ldx + first;
-  const T* up = a.residual ? a.residual + r * a.ldr + first : nullptr;
-  T* yp = a.y + r * a.ldy + first;
-  T* sp = a.sum_out ? a.sum_out + r * a.lds + first : nullptr;
+  const T* xp = a.x + r * a.ldx;
+  const T* up = a.residual ? a.residual + r * a.ldr : nullptr;
+  T* yp = a.y + r * a.ldy;
+  T* sp = a.sum_out ? a.sum_out + r * a.lds : nullptr;
   long long code = r * s.width + first, scale = r * s.scale_pitch + (first >> 5);
   const int pad = (first & 31) == 0 ? -s.groups & 3 : 0;
   Raw8<T> x[K], u[K];
   auto load = [&](bool live) {
+    const int cols = live ? s.cols : 0;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      x[k].zero();
-      u[k].zero();
-      if (live && first + k * apart_by < s.cols) {
-        x[k].load(xp + k * apart_by);
-        if (up) u[k].load(up + k * apart_by);
-      }
+      x[k] = load_chunk<T, VEC>(xp, first + k * apart_by, cols);
+      if (up) u[k] = load_chunk<T, VEC>(up, first + k * apart_by, cols);
     }
   };
   load(r < s.rows);
@@ -186,10 +184,16 @@ __global__ void __launch_bounds__(kForwardThreads<K>, 1) forward_vec_kernel(Forw
     part = two(0.f);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      if (first + k * apart_by >= s.cols) continue;
+      const int left = s.cols - (first + k * apart_by);
+      if (left <= 0) continue;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const F2 d = add2(v[k][j], minus_mean);
+        F2 d = add2(v[k][j], minus_mean);
+        if (!VEC && left < 2 * j + 2) {                   // past the row's end: zeros that count as nothing
+          float lo, hi;
+          apart(d, &lo, &hi);
+          d = two(left > 2 * j ? lo : 0.f, 0.f);
+        }
         part = fma2(d, d, part);
       }
     }
@@ -203,26 +207,33 @@ __global__ void __launch_bounds__(kForwardThreads<K>, 1) forward_vec_kernel(Forw
     const F2 rstd2 = two(rstd);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int at = first + k * apart_by, g = at >> 5;
-      const bool in = at < s.cols, keep = live && g < s.groups;
+      const int at = first + k * apart_by, g = at >> 5, left = s.cols - at;
+      const bool keep = live && g < s.groups;
       Raw8<T> raw;
       if (sp || a.ck_sum.codes) {
         raw.put(v[k]);
-        if (live && in && sp) raw.store(sp + k * apart_by);
+        if (sp) store_chunk<T, VEC>(sp, at, s.cols, raw, live, prev, next);
         if (a.ck_sum.codes)               // the values as they are stored
           act8_put(a.ck_sum.codes + code + k * apart_by, a.ck_sum.scales + scale + k * (apart_by >> 5), raw, (at & 31) == 0,
                    g == s.groups - 1 ? pad : 0, keep);
       }
       raw.zero();
-      if (in) {
+      if (left > 0) {
         F2 w[4], b[4];
         weight.get(at >> 3, w);
         bias.get(at >> 3, b);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[k][j] = fma2(mul2(add2(v[k][j], minus_mean), rstd2), w[j], b[j]);
+        for (int j = 0; j < 4; ++j) {
+          v[k][j] = fma2(mul2(add2(v[k][j], minus_mean), rstd2), w[j], b[j]);
+          if (!VEC && left < 2 * j + 2) {
+            float lo, hi;
+            apart(v[k][j], &lo, &hi);
+            v[k][j] = two(left > 2 * j ? lo : 0.f, 0.f);
+          }
+        }
         raw.put(v[k]);
-        if (live) raw.store(yp + k * apart_by);
       }
+      store_chunk<T, VEC>(yp, at, s.cols, raw, live, prev, next);
       if (a.ck_y.codes)
         act8_put(a.ck_y.codes + code + k * apart_by, a.ck_y.scales + scale + k * (apart_by >> 5), raw, (at & 31) == 0,
                  g == s.groups - 1 ? pad : 0, keep);
@@ -235,101 +246,19 @@ __global__ void __launch_bounds__(kForwardThreads<K>, 1) forward_vec_kernel(Forw
   }
 }
 
-// Rows of any alignment, element by element.
-template <typename T, int K>
-__global__ void __launch_bounds__(kForwardThreads<K>, 1) forward_kernel(Forward<T> a, Shape s) {
-  constexpr bool VEC = false;
-  __shared__ TeamSums<1> buf;
-  clear_sums(buf);
-  int phase = 0;
-  const int teams = blockDim.x / s.team, t = threadIdx.x % s.team, mine = threadIdx.x / s.team;
-  const long long stride = (long long)gridDim.x * teams;
-  const long long turns = (s.rows + stride - 1) / stride;       // the same for every thread: all take part in the sums
-  long long r = (long long)blockIdx.x * teams + mine;
-  Raw8<T> x[K], u[K];
-  auto load = [&](long long row) {
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const Place<VEC> p(t, s.team, k);
-      x[k] = load_chunk<T, VEC>(a.x + row * a.ldx, p, row < s.rows ? s.cols : 0);
-      if (a.residual) u[k] = load_chunk<T, VEC>(a.residual + row * a.ldr, p, row < s.rows ? s.cols : 0);
-    }
-  };
-  for (long long i = 0; i < turns; ++i, r += stride) {
-    load(r);                              // (two rows at once would not fit the registers)
-    const bool live = r < s.rows;
-    float v[K][8];
-    float sum[1] = {0.f};
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      x[k].get(v[k]);
-      if (a.residual) {
-        float w[8];
-        u[k].get(w);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[k][j] += w[j];
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) sum[0] += v[k][j];
-    }
-    team_sum(sum, s.team, buf, &phase);
-    const float mean = mean_of(sum[0], s);
-    sum[0] = 0.f;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const Place<VEC> p(t, s.team, k);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float d = p.at(j) < s.cols ? v[k][j] - mean : 0.f;
-        sum[0] = fmaf(d, d, sum[0]);
-      }
-    }
-    team_sum(sum, s.team, buf, &phase);
-    const float rstd = rsqrtf(mean_of(sum[0], s) + a.eps);
-    if (live && t == 0) {
-      if (a.mean) a.mean[r] = mean;
-      if (a.rstd) a.rstd[r] = rstd;
-    }
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const Place<VEC> p(t, s.team, k);
-      float w[8], b[8], y[8];
-      load_param<VEC>(a.weight, p, s.cols, 1.f, w);
-      load_param<VEC>(a.bias, p, s.cols, 0.f, b);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = fmaf((v[k][j] - mean) * rstd, w[j], b[j]);
-      if (live) {
-        if (a.sum_out) store_chunk<T, VEC>(a.sum_out + r * a.lds, p, s.cols, v[k]);
-        store_chunk<T, VEC>(a.y + r * a.ldy, p, s.cols, y);
-      }
-      const size_t code_row = (size_t)(live ? r : 0) * s.width, scale_row = (size_t)(live ? r : 0) * s.scale_pitch;
-      if (a.ck_sum.codes) {               // checkpoints hold the values as they are stored
-        round_to<T>(v[k]);
-        act8_put<VEC>(a.ck_sum.codes + code_row, a.ck_sum.scales + scale_row, p, s.groups, v[k], live);
-      }
-      if (a.ck_y.codes) {
-        round_to<T>(y);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = p.at(j) < s.cols ? y[j] : 0.f;   // past the row's end: (0 - mean) rstd
-        act8_put<VEC>(a.ck_y.codes + code_row, a.ck_y.scales + scale_row, p, s.groups, y, live);
-      }
-    }
-  }
-}
-
 // Rows of any length: one block per row, three reads.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kBlock) forward_long_kernel(Forward<T> a, Shape s) {
   __shared__ TeamSums<1> buf;
   clear_sums(buf);
   int phase = 0;
-  const int turns = (s.width / 8 + kBlock - 1) / kBlock;
+  const int turns = (s.width / 8 + kBlock - 1) / kBlock, lane = threadIdx.x & 31;
   for (long long r = blockIdx.x; r < s.rows; r += gridDim.x) {
-    auto value = [&](const Place<VEC>& p, float (&v)[8]) {
-      load_chunk<T, VEC>(a.x + r * a.ldx, p, s.cols).get(v);
+    auto value = [&](int first, float (&v)[8]) {
+      load_chunk<T, VEC>(a.x + r * a.ldx, first, s.cols).get(v);
       if (a.residual) {
         float u[8];
-        load_chunk<T, VEC>(a.residual + r * a.ldr, p, s.cols).get(u);
+        load_chunk<T, VEC>(a.residual + r * a.ldr, first, s.cols).get(u);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] += u[j];
       }
@@ -337,7 +266,7 @@ __global__ void __launch_bounds__(kBlock) forward_long_kernel(Forward<T> a, Shap
     float sum[1] = {0.f};
     for (int i = 0; i < turns; ++i) {
       float v[8];
-      value(Place<VEC>(threadIdx.x, kBlock, i), v);
+      value((threadIdx.x + i * kBlock) * 8, v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) sum[0] += v[j];
     }
@@ -345,12 +274,12 @@ __global__ void __launch_bounds__(kBlock) forward_long_kernel(Forward<T> a, Shap
     const float mean = mean_of(sum[0], s);
     sum[0] = 0.f;
     for (int i = 0; i < turns; ++i) {
-      const Place<VEC> p(threadIdx.x, kBlock, i);
+      const int first = (threadIdx.x + i * kBlock) * 8;
       float v[8];
-      value(p, v);
+      value(first, v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float d = p.at(j) < s.cols ? v[j] - mean : 0.f;
+        const float d = first + j < s.cols ? v[j] - mean : 0.f;
         sum[0] = fmaf(d, d, sum[0]);
       }
     }
@@ -361,24 +290,22 @@ __global__ void __launch_bounds__(kBlock) forward_long_kernel(Forward<T> a, Shap
       if (a.rstd) a.rstd[r] = rstd;
     }
     for (int i = 0; i < turns; ++i) {
-      const Place<VEC> p(threadIdx.x, kBlock, i);
+      const int first = (threadIdx.x + i * kBlock) * 8, g = first >> 5;
+      const int pad = g == s.groups - 1 ? -s.groups & 3 : 0;
       float v[8], w[8], b[8], y[8];
-      value(p, v);
-      load_param<VEC>(a.weight, p, s.cols, 1.f, w);
-      load_param<VEC>(a.bias, p, s.cols, 0.f, b);
+      value(first, v);
+      load_param(a.weight, first, s.cols, 1.f, w);
+      load_param(a.bias, first, s.cols, 0.f, b);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = p.at(j) < s.cols ? fmaf((v[j] - mean) * rstd, w[j], b[j]) : 0.f;
-      if (a.sum_out) store_chunk<T, VEC>(a.sum_out + r * a.lds, p, s.cols, v);
-      store_chunk<T, VEC>(a.y + r * a.ldy, p, s.cols, y);
-      const size_t code_row = (size_t)r * s.width, scale_row = (size_t)r * s.scale_pitch;
-      if (a.ck_sum.codes) {
-        round_to<T>(v);
-        act8_put<VEC>(a.ck_sum.codes + code_row, a.ck_sum.scales + scale_row, p, s.groups, v, true);
-      }
-      if (a.ck_y.codes) {
-        round_to<T>(y);
-        act8_put<VEC>(a.ck_y.codes + code_row, a.ck_y.scales + scale_row, p, s.groups, y, true);
-      }
+      for (int j = 0; j < 8; ++j) y[j] = first + j < s.cols ? fmaf((v[j] - mean) * rstd, w[j], b[j]) : 0.f;
+      Raw8<T> rs, ry;
+      rs.put(v);
+      ry.put(y);
+      if (a.sum_out) store_chunk<T, VEC>(a.sum_out + r * a.lds, first, s.cols, rs, true, lane > 0, lane < 31);
+      store_chunk<T, VEC>(a.y + r * a.ldy, first, s.cols, ry, true, lane > 0, lane < 31);
+      const long long code = r * s.width + first, scale = r * s.scale_pitch + g;
+      if (a.ck_sum.codes) act8_put(a.ck_sum.codes + code, a.ck_sum.scales + scale, rs, (first & 31) == 0, pad, g < s.groups);
+      if (a.ck_y.codes) act8_put(a.ck_y.codes + code, a.ck_y.scales + scale, ry, (first & 31) == 0, pad, g < s.groups);
     }
   }
 }
@@ -400,112 +327,117 @@ struct Backward {
 template <typename T, bool VEC, bool CK>
 struct Input {
   Raw8<T> x;
-  __device__ __forceinline__ void load(const Backward<T>& a, const Shape& s, long long r, const Place<VEC>& p, bool live) {
-    x = load_chunk<T, VEC>(a.x + r * a.ldx, p, live ? s.cols : 0);
+  // the first `cols` elements of row r exist
+  __device__ __forceinline__ void load(const Backward<T>& a, const Shape&, long long r, int first, int cols) {
+    x = load_chunk<T, VEC>(a.x + r * a.ldx, first, cols);
   }
-  __device__ __forceinline__ void get(float (&v)[8]) const { x.get(v); }
+  template <typename V> __device__ __forceinline__ void get(V& v) const { x.get(v); }
 };
 template <typename T, bool VEC>
 struct Input<T, VEC, true> {
-  RawAct8<VEC> x;
-  __device__ __forceinline__ void load(const Backward<T>& a, const Shape& s, long long r, const Place<VEC>& p, bool live) {
-    x.load(a.ck.codes + (size_t)r * s.width, a.ck.scales + (size_t)r * s.scale_pitch, p, live ? s.groups : 0);
+  RawAct8 x;
+  __device__ __forceinline__ void load(const Backward<T>& a, const Shape& s, long long r, int first, int cols) {
+    x.load(a.ck.codes + r * s.width + first, a.ck.scales + r * s.scale_pitch + (first >> 5), first < cols);
   }
-  __device__ __forceinline__ void get(float (&v)[8]) const { x.get(v); }
+  __device__ __forceinline__ void get(F2 (&v)[4]) const { x.get(v); }
 };
 
-// The block's column sums (thread t of a team: element j of chunk k) into its partial sums.  `dyn`: [teams - 1] of
-// the team's values, element j of chunk k of thread t at (k * 8 + j) * team + t: neighbouring threads, neighbouring words.
-template <bool VEC, int K>
+// The block's column sums (thread t of a team: chunks t + k * team) into its partial sums.  `dyn`: [teams - 1] of the
+// team's values, element j of chunk k of thread t at (k * 8 + j) * team + t: neighbouring threads, neighbouring words.
+template <int K>
 __device__ __forceinline__ void write_partials(float* out, float* dyn, const Shape& s, int teams, int t, int mine,
-                                               const float (&dw)[K][8], const float (&db)[K][8]) {
+                                               const F2 (&dw)[K][4], const F2 (&db)[K][4]) {
   const int all = s.team * 8 * K;
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
+    float v[K][8];
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) apart(half ? db[k][j] : dw[k][j], &v[k][2 * j], &v[k][2 * j + 1]);
     if (teams > 1) {
       __syncthreads();
       if (mine > 0) {
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) dyn[(mine - 1) * all + (k * 8 + j) * s.team + t] = half ? db[k][j] : dw[k][j];
+          for (int j = 0; j < 8; ++j) dyn[(mine - 1) * all + (k * 8 + j) * s.team + t] = v[k][j];
       }
       __syncthreads();
     }
     if (mine > 0) continue;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const Place<VEC> p(t, s.team, k);
-      float v[8];
+      const int first = (t + k * s.team) * 8;
+      if (first >= s.width) continue;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        v[j] = half ? db[k][j] : dw[k][j];
-        for (int q = 0; q < teams - 1; ++q) v[j] += dyn[q * all + (k * 8 + j) * s.team + t];
-      }
-      store_chunk<float, VEC>(out + half * s.width, p, s.width, v);
+      for (int j = 0; j < 8; ++j)
+        for (int q = 0; q < teams - 1; ++q) v[k][j] += dyn[q * all + (k * 8 + j) * s.team + t];
+      Raw8<float> o;
+      o.put(v[k]);
+      o.store(out + half * s.width + first);
     }
   }
 }
 
-// Persistent: a team walks over rows, its share of the column sums stays in registers.  For rows that 16-byte loads
-// can address; two values per instruction as in the forward pass.
-template <typename T, int K, bool CK>
-__global__ void __launch_bounds__((kBackwardThreads<T, K>), 1) backward_vec_kernel(Backward<T> a, Shape s) {
+// Persistent: a team walks over rows, its share of the column sums stays in registers.
+template <typename T, bool VEC, int K, bool CK>
+__global__ void __launch_bounds__((kBackwardThreads<T, K>), 1) backward_kernel(Backward<T> a, Shape s) {
   extern __shared__ float4 dyn4[];          // the weight; then the column sums of the block's other teams
   float* dyn = reinterpret_cast<float*>(dyn4) + s.width;
   const ParamCache weight = cache_param(reinterpret_cast<float*>(dyn4), a.weight, s, 1.f);
   __shared__ TeamSums<2> buf;
   clear_sums(buf);
   int phase = 0;
-  const int teams = blockDim.x / s.team, t = threadIdx.x % s.team, mine = threadIdx.x / s.team;
+  const int teams = blockDim.x / s.team, t = threadIdx.x % s.team, mine = threadIdx.x / s.team, lane = threadIdx.x & 31;
+  const bool prev = lane > 0 && t > 0, next = lane < 31 && t + 1 < s.team;
   const long long stride = (long long)gridDim.x * teams;
   const int turns = static_cast<int>((s.rows + stride - 1) / stride);
   long long r = (long long)blockIdx.x * teams + mine;
   const int first = t * 8, apart_by = s.team * 8;
-  const T* dyp = a.dy + r * a.lddy + first;
-  const T* xp = CK ? nullptr : a.x + r * a.ldx + first;
+  const T* dyp = a.dy + r * a.lddy;
+  const T* xp = CK ? nullptr : a.x + r * a.ldx;
   const uint8_t* codes = CK ? a.ck.codes + r * s.width + first : nullptr;
   const uint8_t* scales = CK ? a.ck.scales + r * s.scale_pitch + (first >> 5) : nullptr;
-  const T* up = a.residual ? a.residual + r * a.ldr + first : nullptr;
-  T* dxp = a.dx + r * a.lddx + first;
+  const T* up = a.residual ? a.residual + r * a.ldr : nullptr;
+  T* dxp = a.dx + r * a.lddx;
   F2 dw[K][4], db[K][4];
 #pragma unroll
   for (int k = 0; k < K; ++k)
 #pragma unroll
     for (int j = 0; j < 4; ++j) dw[k][j] = db[k][j] = two(0.f);
+  constexpr bool kResidualAhead = sizeof(T) == 2 || K == 1;        // (more fp32 rows ahead would not fit the registers)
   Raw8<T> in_dy[K], in_x[CK ? 1 : K], in_u[K], next_u[K];
-  RawAct8<true> in_q[CK ? K : 1];
+  RawAct8 in_q[CK ? K : 1];
   float mean = 0.f, rstd = 0.f;
   auto load = [&](long long row) {
     const bool live = row < s.rows;
+    const int cols = live ? s.cols : 0;
     mean = live ? a.mean[row] : 0.f;
     rstd = live ? a.rstd[row] : 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const bool in = live && first + k * apart_by < s.cols;
-      in_dy[k].zero();
-      if (in) in_dy[k].load(dyp + k * apart_by);
-      if constexpr (CK) {
-        if (in) {
-          in_q[k].q = *reinterpret_cast<const uint2*>(codes + k * apart_by);
-          in_q[k].byte = scales[k * (apart_by >> 5)];
-        }
-      } else {
-        if (in) in_x[k].load(xp + k * apart_by);
-      }
-      if (in && up) next_u[k].load(up + k * apart_by);
+      const int at = first + k * apart_by;
+      in_dy[k] = load_chunk<T, VEC>(dyp, at, cols);
+      if constexpr (CK) in_q[k].load(codes + k * apart_by, scales + k * (apart_by >> 5), at < cols);
+      else in_x[k] = load_chunk<T, VEC>(xp, at, cols);
+      if (kResidualAhead && up) next_u[k] = load_chunk<T, VEC>(up, at, cols);
     }
   };
   load(r);
   for (int i = 0; i < turns; ++i) {
     const bool live = r < s.rows;
 #pragma unroll
-    for (int k = 0; k < K; ++k) in_u[k] = next_u[k];
+    for (int k = 0; k < K; ++k) {
+      if (kResidualAhead) in_u[k] = next_u[k];
+      else if (up) in_u[k] = load_chunk<T, VEC>(up, first + k * apart_by, live ? s.cols : 0);
+    }
     const F2 rstd2 = two(rstd), minus_mean = two(-mean);
     F2 g[K][4], h[K][4], sg = two(0.f), sgh = two(0.f);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      if (!live || first + k * apart_by >= s.cols) {
+      const int left = live ? s.cols - (first + k * apart_by) : 0;
+      if (left <= 0) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) g[k][j] = h[k][j] = two(0.f);
         continue;
@@ -517,6 +449,7 @@ __global__ void __launch_bounds__((kBackwardThreads<T, K>), 1) backward_vec_kern
       else in_x[k].get(h[k]);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
+        // (past the row's end dy is zero, and h only ever meets it or is not stored)
         h[k][j] = mul2(add2(h[k][j], minus_mean), rstd2);
         g[k][j] = mul2(dy[j], w[j]);
         sg = add2(sg, g[k][j]);
@@ -539,7 +472,6 @@ __global__ void __launch_bounds__((kBackwardThreads<T, K>), 1) backward_vec_kern
     const F2 mg = two(-sum[0] * s.inv), mgh = two(-sum[1] * s.inv);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      if (!live || first + k * apart_by >= s.cols) continue;
 #pragma unroll
       for (int j = 0; j < 4; ++j) g[k][j] = mul2(fma2(h[k][j], mgh, add2(g[k][j], mg)), rstd2);
       if (a.residual) {
@@ -550,101 +482,12 @@ __global__ void __launch_bounds__((kBackwardThreads<T, K>), 1) backward_vec_kern
       }
       Raw8<T> o;
       o.put(g[k]);
-      o.store(dxp + k * apart_by);
+      store_chunk<T, VEC>(dxp, first + k * apart_by, s.cols, o, live, prev, next);
     }
     r += stride;
     dxp += stride * a.lddx;
   }
-  if (!a.partials) return;
-  float fw[K][8], fb[K][8];
-#pragma unroll
-  for (int k = 0; k < K; ++k)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      apart(dw[k][j], &fw[k][2 * j], &fw[k][2 * j + 1]);
-      apart(db[k][j], &fb[k][2 * j], &fb[k][2 * j + 1]);
-    }
-  write_partials<true, K>(a.partials + (size_t)blockIdx.x * 2 * s.width, dyn, s, teams, t, mine, fw, fb);
-}
-
-// Rows of any alignment, element by element.
-template <typename T, int K, bool CK>
-__global__ void __launch_bounds__((kBackwardThreads<T, K>), 1) backward_kernel(Backward<T> a, Shape s) {
-  constexpr bool VEC = false;
-  extern __shared__ float dyn[];
-  __shared__ TeamSums<2> buf;
-  clear_sums(buf);
-  int phase = 0;
-  const int teams = blockDim.x / s.team, t = threadIdx.x % s.team, mine = threadIdx.x / s.team;
-  const long long stride = (long long)gridDim.x * teams;
-  const long long turns = (s.rows + stride - 1) / stride;
-  float dw[K][8], db[K][8];
-#pragma unroll
-  for (int k = 0; k < K; ++k)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) dw[k][j] = db[k][j] = 0.f;
-  long long r = (long long)blockIdx.x * teams + mine;
-  Raw8<T> in_dy[K], in_r[K];
-  Input<T, VEC, CK> in_x[K];
-  float mean = 0.f, rstd = 0.f;
-  auto load = [&](long long row) {
-    const bool live = row < s.rows;
-    mean = live ? a.mean[row] : 0.f;
-    rstd = live ? a.rstd[row] : 0.f;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const Place<VEC> p(t, s.team, k);
-      in_dy[k] = load_chunk<T, VEC>(a.dy + row * a.lddy, p, live ? s.cols : 0);
-      in_x[k].load(a, s, row, p, live);
-    }
-  };
-  for (long long i = 0; i < turns; ++i, r += stride) {
-    load(r);
-    const bool live = r < s.rows;
-    const float row_rstd = rstd;
-    Raw8<T> dyr[K];
-    float h[K][8];
-    float sum[2] = {0.f, 0.f};
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const Place<VEC> p(t, s.team, k);
-      float w[8], dy[8];
-      load_param<VEC>(a.weight, p, s.cols, 1.f, w);
-      dyr[k] = in_dy[k];
-      in_dy[k].get(dy);
-      in_x[k].get(h[k]);
-      if (a.residual) in_r[k] = load_chunk<T, VEC>(a.residual + r * a.ldr, p, live ? s.cols : 0);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        h[k][j] = p.at(j) < s.cols ? (h[k][j] - mean) * rstd : 0.f;
-        const float g = dy[j] * w[j];
-        sum[0] += g;
-        sum[1] = fmaf(g, h[k][j], sum[1]);
-        dw[k][j] = fmaf(dy[j], h[k][j], dw[k][j]);
-        db[k][j] += dy[j];
-      }
-    }
-    team_sum(sum, s.team, buf, &phase);
-    const float mg = mean_of(sum[0], s), mgh = mean_of(sum[1], s);
-    if (!live) continue;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const Place<VEC> p(t, s.team, k);
-      float w[8], dy[8], o[8];
-      load_param<VEC>(a.weight, p, s.cols, 1.f, w);
-      dyr[k].get(dy);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] = row_rstd * (fmaf(dy[j], w[j], -mg) - h[k][j] * mgh);
-      if (a.residual) {
-        float u[8];
-        in_r[k].get(u);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] += u[j];
-      }
-      store_chunk<T, VEC>(a.dx + r * a.lddx, p, s.cols, o);
-    }
-  }
-  if (a.partials) write_partials<VEC, K>(a.partials + (size_t)blockIdx.x * 2 * s.width, dyn, s, teams, t, mine, dw, db);
+  if (a.partials) write_partials<K>(a.partials + (size_t)blockIdx.x * 2 * s.width, dyn, s, teams, t, mine, dw, db);
 }
 
 // Long rows, first step: mean(g) and mean(g h) of every row.
@@ -658,18 +501,21 @@ __global__ void __launch_bounds__(kBlock) backward_stats_kernel(Backward<T> a, S
     const float mean = a.mean[r], rstd = a.rstd[r];
     float sum[2] = {0.f, 0.f};
     for (int i = 0; i < turns; ++i) {
-      const Place<VEC> p(threadIdx.x, kBlock, i);
+      const int first = (threadIdx.x + i * kBlock) * 8;
       Input<T, VEC, CK> in;
+      F2 v2[4];
       float dy[8], v[8], w[8];
-      in.load(a, s, r, p, true);
-      load_chunk<T, VEC>(a.dy + r * a.lddy, p, s.cols).get(dy);
-      in.get(v);
-      load_param<VEC>(a.weight, p, s.cols, 1.f, w);
+      in.load(a, s, r, first, s.cols);
+      load_chunk<T, VEC>(a.dy + r * a.lddy, first, s.cols).get(dy);
+      in.get(v2);
+      load_param(a.weight, first, s.cols, 1.f, w);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int j = 0; j < 4; ++j) apart(v2[j], &v[2 * j], &v[2 * j + 1]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {        // (past the row's end dy is zero)
         const float g = dy[j] * w[j];
         sum[0] += g;
-        sum[1] = fmaf(g, p.at(j) < s.cols ? (v[j] - mean) * rstd : 0.f, sum[1]);
+        sum[1] = first + j < s.cols ? fmaf(g, (v[j] - mean) * rstd, sum[1]) : sum[1];
       }
     }
     team_sum(sum, kBlock, buf, &phase);
@@ -685,31 +531,36 @@ template <typename T, bool VEC, bool CK>
 __global__ void __launch_bounds__(256) backward_long_kernel(Backward<T> a, Shape s, const float* stats) {
   __shared__ float part[8][8 * 33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const Place<VEC> p(lane, 32, blockIdx.y);
+  const int first = (blockIdx.y * 32 + lane) * 8;
   float dw[8], db[8], w[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) dw[j] = db[j] = 0.f;
-  load_param<VEC>(a.weight, p, s.cols, 1.f, w);
+  load_param(a.weight, first, s.cols, 1.f, w);
   for (long long r = (long long)blockIdx.x * 8 + warp; r < s.rows; r += (long long)gridDim.x * 8) {
     const float mean = a.mean[r], rstd = a.rstd[r], mg = stats[2 * r], mgh = stats[2 * r + 1];
     Input<T, VEC, CK> in;
+    F2 v2[4];
     float dy[8], v[8], o[8];
-    in.load(a, s, r, p, true);
-    load_chunk<T, VEC>(a.dy + r * a.lddy, p, s.cols).get(dy);
-    in.get(v);
+    in.load(a, s, r, first, s.cols);
+    load_chunk<T, VEC>(a.dy + r * a.lddy, first, s.cols).get(dy);
+    in.get(v2);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) apart(v2[j], &v[2 * j], &v[2 * j + 1]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float h = p.at(j) < s.cols ? (v[j] - mean) * rstd : 0.f;
+      const float h = first + j < s.cols ? (v[j] - mean) * rstd : 0.f;
       o[j] = rstd * (fmaf(dy[j], w[j], -mg) - h * mgh);
       dw[j] = fmaf(dy[j], h, dw[j]);
       db[j] += dy[j];
     }
     if (a.residual) {
-      load_chunk<T, VEC>(a.residual + r * a.ldr, p, s.cols).get(v);
+      load_chunk<T, VEC>(a.residual + r * a.ldr, first, s.cols).get(v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) o[j] += v[j];
     }
-    store_chunk<T, VEC>(a.dx + r * a.lddx, p, s.cols, o);
+    Raw8<T> raw;
+    raw.put(o);
+    store_chunk<T, VEC>(a.dx + r * a.lddx, first, s.cols, raw, true, lane > 0, lane < 31);
   }
   if (!a.partials) return;
   float* out = a.partials + (size_t)blockIdx.x * 2 * s.width;
@@ -718,8 +569,7 @@ __global__ void __launch_bounds__(256) backward_long_kernel(Backward<T> a, Shape
 #pragma unroll
     for (int j = 0; j < 8; ++j) part[warp][j * 33 + lane] = half ? db[j] : dw[j];
     __syncthreads();
-    // column threadIdx.x of the block: VEC element % 8 of lane / 8, otherwise element / 32 of lane % 32
-    const int j = VEC ? threadIdx.x & 7 : threadIdx.x >> 5, l = VEC ? threadIdx.x >> 3 : threadIdx.x & 31;
+    const int j = threadIdx.x & 7, l = threadIdx.x >> 3;
     const int col = blockIdx.y * 256 + threadIdx.x;
     if (col < s.width) {
       float v = 0.f;
@@ -779,7 +629,7 @@ template <typename T, bool VEC>
 cudaError_t ln_forward_t(const ln::Forward<T>& a, long long rows, long long cols, cudaStream_t st) {
   ln::Shape s = ln_shape(rows, cols);
   int K = 1;
-  const int few = VEC && sizeof(T) == 2 ? 4 : 1, many = VEC && sizeof(T) == 2 ? 4 : 2;
+  const int few = sizeof(T) == 2 ? 4 : 1, many = sizeof(T) == 2 ? 4 : 2;
   if (!ln_team(&s, VEC, few, many, ln::kMaxKForward, &K)) {
     const unsigned grid = static_cast<unsigned>(rows < (1 << 30) ? rows : 1 << 30);
     ln::forward_long_kernel<T, VEC><<<grid, ln::kBlock, 0, st>>>(a, s);
@@ -788,22 +638,15 @@ cudaError_t ln_forward_t(const ln::Forward<T>& a, long long rows, long long cols
   const int threads = ln_block(s, K == 1 ? 768 : ln::kBlock), teams = threads / s.team;
   const long long want = (rows + teams - 1) / teams, most = sm_count();
   const unsigned grid = static_cast<unsigned>(want < most ? want : most);
-  const size_t smem = VEC ? 2 * (size_t)s.width * sizeof(float) : 0;
+  const size_t smem = 2 * (size_t)s.width * sizeof(float);
   auto go = [&](auto kernel) {
     if (smem > 32 << 10) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     kernel<<<grid, threads, smem, st>>>(a, s);
   };
-  if constexpr (VEC) {
-    if (K == 1) go(ln::forward_vec_kernel<T, 1>);
-    else if (K == 2) go(ln::forward_vec_kernel<T, 2>);
-    else if (K == 3) go(ln::forward_vec_kernel<T, 3>);
-    else go(ln::forward_vec_kernel<T, 4>);
-  } else {
-    if (K == 1) go(ln::forward_kernel<T, 1>);
-    else if (K == 2) go(ln::forward_kernel<T, 2>);
-    else if (K == 3) go(ln::forward_kernel<T, 3>);
-    else go(ln::forward_kernel<T, 4>);
-  }
+  if (K == 1) go(ln::forward_kernel<T, VEC, 1>);
+  else if (K == 2) go(ln::forward_kernel<T, VEC, 2>);
+  else if (K == 3) go(ln::forward_kernel<T, VEC, 3>);
+  else go(ln::forward_kernel<T, VEC, 4>);
   return cudaGetLastError();
 }
 
@@ -814,7 +657,7 @@ cudaError_t ln_forward_d(Mat x, Mat residual, long long rows, long long cols, Pa
   ln::Forward<T> a{};
   a.x = row_of<T>(x, 0); a.ldx = x.ld;
   a.residual = row_of<T>(residual, 0); a.ldr = residual.ld;
-  a.weight = param_vec(weight, cols); a.bias = param_vec(bias, cols);
+  a.weight = param_vec(weight); a.bias = param_vec(bias);
   a.eps = eps;
   a.y = row_of<T>(y, 0); a.ldy = y.ld;
   a.sum_out = row_of<T>(sum_out, 0); a.lds = sum_out.ld;
@@ -859,19 +702,14 @@ cudaError_t ln_backward_t(const ln::Backward<T>& a, const LnBackwardGrid& g, flo
     const dim3 grid(g.grid, (g.s.width + 255) / 256);
     ln::backward_long_kernel<T, VEC, CK><<<grid, 256, 0, st>>>(a, g.s, row_stats);
   } else {
-    const size_t smem = (VEC ? (size_t)g.s.width * sizeof(float) : 0) +
+    const size_t smem = (size_t)g.s.width * sizeof(float) +
                         (a.partials ? (size_t)(g.teams - 1) * g.s.team * 8 * g.K * sizeof(float) : 0);
     auto go = [&](auto kernel) {
       if (smem > 32 << 10) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
       kernel<<<g.grid, g.threads, smem, st>>>(a, g.s);
     };
-    if constexpr (VEC) {
-      if (g.K == 1) go(ln::backward_vec_kernel<T, 1, CK>);
-      else go(ln::backward_vec_kernel<T, 2, CK>);
-    } else {
-      if (g.K == 1) go(ln::backward_kernel<T, 1, CK>);
-      else go(ln::backward_kernel<T, 2, CK>);
-    }
+    if (g.K == 1) go(ln::backward_kernel<T, VEC, 1, CK>);
+    else go(ln::backward_kernel<T, VEC, 2, CK>);
   }
   return cudaGetLastError();
 }
@@ -888,7 +726,7 @@ cudaError_t ln_backward_d(Mat dy, Mat x, const void* ck, long long rows, long lo
     a.dy = row_of<T>(dy, 0); a.lddy = dy.ld;
     a.x = row_of<T>(x, 0); a.ldx = x.ld;
     a.ck = act8_at(ck, rows, cols, 0);
-    a.weight = param_vec(weight, cols);
+    a.weight = param_vec(weight);
     a.mean = mean; a.rstd = rstd;
     a.residual = row_of<T>(residual, 0); a.ldr = residual.ld;
     a.dx = row_of<T>(dx, 0); a.lddx = dx.ld;

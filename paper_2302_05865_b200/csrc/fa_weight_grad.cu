@@ -253,7 +253,7 @@ struct ColumnSums {
           const long long row = row0 + q * 8;
           if (h < halves && row < p.rows) {
             if (col + 8 <= p.outs) r[q].load(src + row * p.ld + col);
-            else if (col < p.outs) r[q] = load_chunk<bf16, false>(src + row * p.ld + col, Place<false>(0, 1, 0), p.outs - col);
+            else if (col < p.outs) r[q] = load_some(src + row * p.ld + col, p.outs - col);
           }
         }
       };
@@ -590,14 +590,13 @@ __global__ void __launch_bounds__(256) finish_kernel(Finish f) {
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ dy, long long ld, long long rows, int outs,
                                                    int pitch, int planes, bf16* __restrict__ out) {
-  const int per_row = VEC ? pitch / 8 : (outs + 255) / 256 * 32;
+  const int per_row = pitch / 8;
   const long long n = rows * per_row, plane = rows * pitch;
   for (long long j = (long long)blockIdx.x * 256 + threadIdx.x; j < n; j += (long long)gridDim.x * 256) {
     const long long r = j / per_row;
-    const int c = static_cast<int>(j - r * per_row);
-    const Place<VEC> p = VEC ? Place<VEC>(c, 0, 0) : Place<VEC>(c & 31, 32, c >> 5);
+    const int first = static_cast<int>(j - r * per_row) * 8;
     float v[8];
-    load_chunk<T, VEC>(dy + r * ld, p, outs).get(v);
+    load_chunk<T, VEC>(dy + r * ld, first, outs).get(v);
     for (int q = 0; q < planes; ++q) {
       float term[8];
 #pragma unroll
@@ -606,7 +605,9 @@ __global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ dy, lon
         if (isnan(v[k])) term[k] = v[k];
         v[k] = isfinite(v[k]) ? v[k] - term[k] : 0.f;
       }
-      store_chunk<bf16, VEC>(out + q * plane + r * pitch, p, outs, term);
+      Raw8<bf16> o;
+      o.put(term);
+      o.store(out + q * plane + r * pitch + first);
     }
   }
 }
@@ -689,7 +690,7 @@ cudaError_t launch_linear_weight_grad(Mat dy, int dtype, long long rows, long lo
   if (!direct) {
     bf16* packed = static_cast<bf16*>(scratch);
     const bool vec = dtype == FA_F32 && mat_vec<float>(dy, outs);
-    const long long want = (rows * (vec ? p.pitch / 8 : (outs + 255) / 256 * 32) + 255) / 256, most = 16LL * sm_count();
+    const long long want = (rows * (p.pitch / 8) + 255) / 256, most = 16LL * sm_count();
     const unsigned grid = static_cast<unsigned>(want < most ? want : most);
     auto go = [&](auto kernel, auto* src) {
       kernel<<<grid, 256, 0, st>>>(src, dy.ld, rows, (int)outs, p.pitch, p.planes, packed);
