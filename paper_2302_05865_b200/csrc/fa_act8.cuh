@@ -181,36 +181,74 @@ __device__ __forceinline__ void shift_window(uint32_t (&w)[OUT + 4], uint32_t s)
   }
 }
 
-// Elements first .. first + 7 of a row of `cols`, zeros past its end.  VEC: rows start on 16-byte boundaries and cols
-// is a multiple of 8, so a chunk is one aligned load (fp32: two), or lies outside.  Otherwise the chunk is cut out
-// of the aligned 16-byte blocks it lies in, where all of these are inside the row, and read one by one at its ends.
-// (All chunks read one by one, even by neighbouring lanes, took two to four times as long.)
+// A matrix that is read: `end` is where its last row ends.
+template <typename T>
+struct Source {
+  const T* p;
+  long long ld;
+  const T* end;
+};
+
+// Elements first .. first + 7 of a row of `cols`, zeros past its end: fetched now, put together when they are needed, so
+// that a fetch waits for nothing.  VEC: rows start on 16-byte boundaries and cols is a multiple of 8, so a chunk is one
+// aligned load (fp32: two), or lies outside.  Otherwise it is cut out of the aligned 16-byte blocks it lies in, where
+// these are inside the matrix (from its first element to its last, the gaps between rows included); the one or two
+// chunks of a whole matrix where they are not are read element by element.
 template <typename T, bool VEC>
-__device__ __forceinline__ Raw8<T> load_chunk(const T* row, int first, int cols) {
+struct Chunk {
   Raw8<T> r;
-  if constexpr (VEC) {
-    if (first < cols) r.load(row + first);
-    else r.zero();
-  } else {
-    constexpr int kOut = 8 * sizeof(T) / 4, kPer = 16 / sizeof(T);       // words of a chunk, elements of a block
-    const uint32_t s = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row + first)) & 15u;
-    const int before = static_cast<int>(s / sizeof(T));                  // elements of the first block in front of the chunk
-    if (first >= before && first - before + 8 + kPer <= cols) {
-      const uint4* p = reinterpret_cast<const uint4*>(row + first - before);
-      uint32_t w[kOut + 4];
-#pragma unroll
-      for (int i = 0; i < kOut / 4 + 1; ++i) {
-        const uint4 b = p[i];
-        w[4 * i] = b.x; w[4 * i + 1] = b.y; w[4 * i + 2] = b.z; w[4 * i + 3] = b.w;
-      }
-      shift_window<kOut, sizeof(T) == 2>(w, s);
-      r.from_words(w);
-    } else {
-      r = load_some(row + first, cols - first);
-    }
+  // Always a load, of the matrix' first chunk where there is none: around a condition or with a default value the
+  // compiler would not keep several under way.
+  __device__ __forceinline__ void fetch(const Source<T>& m, const T* row, int first, int cols) {
+    r.load(first < cols ? row + first : m.p);
   }
-  return r;
-}
+  // `in`: whether there was one (what it was fetched for); without one, zeros
+  __device__ __forceinline__ Raw8<T> raw(bool in) const {
+    Raw8<T> v = r;
+    if (!in) v.zero();
+    return v;
+  }
+};
+template <typename T>
+struct Chunk<T, false> {
+  static constexpr int kOut = 8 * sizeof(T) / 4, kPer = 16 / sizeof(T);     // words of a chunk, elements of a block
+  uint32_t w[kOut + 4];
+  const T* p;
+  int valid;           // elements of the chunk that exist
+  bool whole;          // its blocks were read
+  __device__ __forceinline__ void fetch(const Source<T>& m, const T* row, int first, int cols) {
+    p = row + first;
+    valid = cols - first;
+    const T* a = p - (static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) & 15u) / sizeof(T);
+    whole = valid > 0 && a >= m.p && a + 8 + kPer <= m.end;
+#pragma unroll
+    for (int i = 0; i < kOut + 4; ++i) w[i] = 0;
+    const uint4* b = reinterpret_cast<const uint4*>(a);
+#pragma unroll
+    for (int i = 0; i < kOut / 4 + 1; ++i)
+      if (whole) {
+        const uint4 t = b[i];
+        w[4 * i] = t.x; w[4 * i + 1] = t.y; w[4 * i + 2] = t.z; w[4 * i + 3] = t.w;
+      }
+  }
+  __device__ __forceinline__ Raw8<T> raw(bool) const {
+    Raw8<T> r;
+    uint32_t v[kOut + 4];
+#pragma unroll
+    for (int i = 0; i < kOut + 4; ++i) v[i] = w[i];
+    shift_window<kOut, sizeof(T) == 2>(v, static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) & 15u);
+    r.from_words(v);
+    if (valid < 8 && valid > 0 && whole) {               // the row ends within the chunk
+      float f[8];
+      r.get(f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = j < valid ? f[j] : 0.f;
+      r.put(f);
+    }
+    if (valid > 0 && !whole) r = load_some(p, valid);
+    return r;
+  }
+};
 
 // The reverse.  All 32 lanes call (not VEC: neighbours complete each other's blocks); `live`: there is something to
 // store; `prev` / `next`: the lane below / above holds the chunk in front / behind, of the same row and live too.
@@ -348,17 +386,13 @@ __device__ __forceinline__ void act8_put(uint8_t* codes, uint8_t* scales, const 
 }
 
 // ---- decode
-// A chunk's codes and its group's scale as they lie in memory; `inside`: the chunk belongs to a group.
+// A chunk's codes and its group's scale as they lie in memory; the first chunk's if it is not `inside`.
 struct RawAct8 {
   uint2 q;
   uint32_t byte;
-  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scale, bool inside) {
-    q = make_uint2(0, 0);
-    byte = 127;
-    if (inside) {
-      q = *reinterpret_cast<const uint2*>(codes);
-      byte = *scale;
-    }
+  __device__ __forceinline__ void load(const Act8& ck, long long code, long long scale, bool inside) {
+    q = *reinterpret_cast<const uint2*>(ck.codes + (inside ? code : 0));
+    byte = ck.scales[inside ? scale : 0];
   }
   __device__ __forceinline__ void get(F2 (&v)[4]) const {
     const F2 s = two(act8_scale(byte)), off = two(-8388736.f);

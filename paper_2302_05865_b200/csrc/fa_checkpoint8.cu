@@ -42,17 +42,19 @@ __device__ __forceinline__ void store_flat(T* out, long long ld, const Flat& f, 
 }
 
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads) store_kernel(const T* __restrict__ x, long long ldx, Act8 ck, Flat f) {
+__global__ void __launch_bounds__(kThreads) store_kernel(Source<T> x, Act8 ck, Flat f) {
   const uint32_t first = blockIdx.x * (kThreads * kPer) + threadIdx.x;
-  Raw8<T> raw[kPer];
+  Chunk<T, VEC> in[kPer];
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const At at(f, first + k * kThreads);
-    raw[k].zero();
-    if (at.valid) raw[k] = load_chunk<T, VEC>(x + at.row * ldx, at.c * 8, f.cols);
+    in[k].fetch(x, x.p + at.row * x.ld, at.c * 8, f.cols);
   }
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) put_chunk(ck, f, At(f, first + k * kThreads), raw[k]);
+  for (int k = 0; k < kPer; ++k) {
+    const At at(f, first + k * kThreads);
+    put_chunk(ck, f, at, in[k].raw(at.c * 8 < f.cols));
+  }
 }
 
 template <typename T, bool VEC>
@@ -62,8 +64,7 @@ __global__ void __launch_bounds__(kThreads) load_kernel(Act8 ck, T* __restrict__
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const At at(f, first + k * kThreads);
-    q[k].load(ck.codes + (size_t)at.row * f.groups * 32 + (size_t)at.c * 8,
-              ck.scales + (size_t)at.row * f.scale_pitch + (at.c >> 2), at.valid);
+    q[k].load(ck, (long long)at.row * f.groups * 32 + at.c * 8, (long long)at.row * f.scale_pitch + (at.c >> 2), true);
   }
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
@@ -150,22 +151,22 @@ __device__ __forceinline__ F2 gelu_slope(float a, float b) {
 }
 
 template <typename T, bool VEC, int APPROX>
-__global__ void __launch_bounds__(kThreads) gelu_forward_kernel(const T* __restrict__ x, long long ldx, ParamVec bias,
+__global__ void __launch_bounds__(kThreads) gelu_forward_kernel(Source<T> x, ParamVec bias,
                                                                 T* __restrict__ y, long long ldy, Act8 ck_x, Act8 ck_y,
                                                                 Flat f) {
   const uint32_t first = blockIdx.x * (kThreads * kPer) + threadIdx.x;
-  Raw8<T> raw[kPer];
+  Chunk<T, VEC> in[kPer];
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const At at(f, first + k * kThreads);
-    raw[k].zero();
-    if (at.valid) raw[k] = load_chunk<T, VEC>(x + at.row * ldx, at.c * 8, f.cols);
+    in[k].fetch(x, x.p + at.row * x.ld, at.c * 8, f.cols);
   }
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const At at(f, first + k * kThreads);
     float z[8], b[8];
-    raw[k].get(z);
+    Raw8<T> raw = in[k].raw(at.c * 8 < f.cols);
+    raw.get(z);
     if (bias.p) {
       load_param(bias, at.c * 8, f.cols, 0.f, b);
 #pragma unroll
@@ -178,16 +179,16 @@ __global__ void __launch_bounds__(kThreads) gelu_forward_kernel(const T* __restr
     }
 #pragma unroll
     for (int j = 0; j < 8; j += 2) gelu<T, APPROX>(z[j], z[j + 1]);
-    raw[k].put(z);
-    store_flat<T, VEC>(y, ldy, f, at, raw[k]);
-    if (ck_y.codes) put_chunk(ck_y, f, at, raw[k]);          // y as it is stored (zeros past the row's end: gelu(0) = 0)
+    raw.put(z);
+    store_flat<T, VEC>(y, ldy, f, at, raw);
+    if (ck_y.codes) put_chunk(ck_y, f, at, raw);          // y as it is stored (zeros past the row's end: gelu(0) = 0)
   }
 }
 
 // ---- column kernels: a thread owns the 8 columns of a chunk and walks over rows; its sums stay in registers.  A block
 // has 256 / lanes rows side by side, `lanes` (a power of two; not VEC: 32, a warp) chunks wide.  Rows are taken kAhead
 // at a time, loads first.
-constexpr int kAhead = 4;
+template <bool VEC> constexpr int kAhead = VEC ? 4 : 2;      // (an unaligned chunk takes more registers on its way)
 struct Columns {
   long long rows;
   int chunks, lanes_log2;
@@ -196,6 +197,7 @@ struct Columns {
 
 template <class Op>
 __global__ void __launch_bounds__(kThreads) column_kernel(Op op, Columns g) {
+  constexpr int kAhead = act8::kAhead<Op::kVec>;
   const int lanes = 1 << g.lanes_log2, side = kThreads >> g.lanes_log2;
   const int rl = threadIdx.x >> g.lanes_log2, lane = threadIdx.x & (lanes - 1);
   const int c = blockIdx.x * lanes + lane;
@@ -232,37 +234,35 @@ __global__ void __launch_bounds__(kThreads) column_kernel(Op op, Columns g) {
 template <typename T, bool VEC, int APPROX, bool CK>
 struct GeluBackward {
   static constexpr bool kVec = VEC;
-  const T* dy; long long lddy;
-  const T* x; long long ldx;
+  Source<T> dy, x;
   ParamVec bias;
   Act8 ck;
   int cols, groups, scale_pitch;
   T* dx; long long lddx;
   float b[8];
   struct In {
-    Raw8<T> dy, x;
+    Chunk<T, VEC> dy, x;
     RawAct8 q;
   };
   __device__ __forceinline__ void begin(int c) {
     if (!CK) load_param(bias, c * 8, cols, 0.f, b);
   }
   __device__ __forceinline__ void load(long long r, int c, In& in) const {
-    in.dy = load_chunk<T, VEC>(dy + r * lddy, c * 8, cols);
+    in.dy.fetch(dy, dy.p + r * dy.ld, c * 8, cols);
     if constexpr (CK)
-      in.q.load(ck.codes + (size_t)r * groups * 32 + (size_t)c * 8, ck.scales + (size_t)r * scale_pitch + (c >> 2),
-                c < groups * 4);
-    else in.x = load_chunk<T, VEC>(x + r * ldx, c * 8, cols);
+      in.q.load(ck, r * groups * 32 + c * 8, r * scale_pitch + (c >> 2), c < groups * 4);
+    else in.x.fetch(x, x.p + r * x.ld, c * 8, cols);
   }
   __device__ __forceinline__ void row(long long r, int c, int lane, const In& in, float (&acc)[8]) const {
     float g[8], z[8];
-    in.dy.get(g);
+    in.dy.raw(c * 8 < cols).get(g);
     if constexpr (CK) {
       F2 v[4];
       in.q.get(v);
 #pragma unroll
       for (int i = 0; i < 4; ++i) apart(v[i], &z[2 * i], &z[2 * i + 1]);
     } else {
-      in.x.get(z);
+      in.x.raw(c * 8 < cols).get(z);
 #pragma unroll
       for (int i = 0; i < 8; ++i) z[i] += b[i];
     }
@@ -353,8 +353,8 @@ template <typename T>
 cudaError_t store_t(Mat x, long long rows, long long cols, void* ck, cudaStream_t st) {
   const bool vec = mat_vec<T>(x, cols);
   return for_flat(rows, cols, [&](unsigned blocks, const act8::Flat& f, long long r0) {
-    if (vec) act8::store_kernel<T, true><<<blocks, act8::kThreads, 0, st>>>(row_of<T>(x, r0), x.ld, act8_at(ck, rows, cols, r0), f);
-    else act8::store_kernel<T, false><<<blocks, act8::kThreads, 0, st>>>(row_of<T>(x, r0), x.ld, act8_at(ck, rows, cols, r0), f);
+    if (vec) act8::store_kernel<T, true><<<blocks, act8::kThreads, 0, st>>>(source_of<T>(x, r0, rows - r0, cols), act8_at(ck, rows, cols, r0), f);
+    else act8::store_kernel<T, false><<<blocks, act8::kThreads, 0, st>>>(source_of<T>(x, r0, rows - r0, cols), act8_at(ck, rows, cols, r0), f);
   });
 }
 template <typename T>
@@ -371,7 +371,7 @@ cudaError_t gelu_forward_t(Mat x, long long rows, long long cols, Param bias, Ma
   const ParamVec b = param_vec(bias);
   return for_flat(rows, cols, [&](unsigned blocks, const act8::Flat& f, long long r0) {
     act8::gelu_forward_kernel<T, VEC, APPROX><<<blocks, act8::kThreads, 0, st>>>(
-        row_of<T>(x, r0), x.ld, b, row_of<T>(y, r0), y.ld, act8_at(ck_x, rows, cols, r0),
+        source_of<T>(x, r0, rows - r0, cols), b, row_of<T>(y, r0), y.ld, act8_at(ck_x, rows, cols, r0),
         act8_at(ck_y, rows, cols, r0), f);
   });
 }
@@ -387,7 +387,7 @@ cudaError_t gelu_forward_d(Mat x, long long rows, long long cols, Param bias, in
 }
 
 // Grid of a column kernel: sixteen blocks per SM, several times what is resident, so that the last ones to run leave
-// little of the GPU idle; but at least two loads ahead (2 * kAhead rows) for every thread as long as there are SMs to fill.
+// little of the GPU idle; but at least eight rows for every thread as long as there are SMs to fill.
 struct ColumnGrid {
   int lanes_log2;
   unsigned x, y;
@@ -403,7 +403,7 @@ ColumnGrid column_grid(bool vec, long long rows, long long cols) {
   const long long x = (g.chunks + lanes - 1) / lanes;
   const long long once = (2LL * sm_count() + x - 1) / x;
   long long y = (16LL * sm_count() + x - 1) / x;
-  const long long full = (rows + side * 2 * act8::kAhead - 1) / (side * 2 * act8::kAhead), most = (rows + side - 1) / side;
+  const long long full = (rows + side * 8 - 1) / (side * 8), most = (rows + side - 1) / side;
   if (y > full) y = full > once ? full : once;
   if (y > most) y = most;
   if (y < 1) y = 1;
@@ -443,8 +443,8 @@ struct GeluBackwardArgs {
 template <typename T, bool VEC, int APPROX, bool CK>
 cudaError_t gelu_backward_t(const GeluBackwardArgs& a, cudaStream_t st) {
   act8::GeluBackward<T, VEC, APPROX, CK> op{};
-  op.dy = row_of<T>(a.dy, 0); op.lddy = a.dy.ld;
-  op.x = row_of<T>(a.x, 0); op.ldx = a.x.ld;
+  op.dy = source_of<T>(a.dy, 0, a.rows, a.cols);
+  op.x = source_of<T>(a.x, 0, a.rows, a.cols);
   op.bias = param_vec(a.bias);
   op.ck = act8_at(a.ck, a.rows, a.cols, 0);
   op.cols = static_cast<int>(a.cols);

@@ -36,4 +36,10 @@ template <typename T> inline T* row_of(const Mat& m, long long row) {
   return m.p ? static_cast<T*>(const_cast<void*>(m.p)) + row * m.ld : nullptr;
 }
 
+template <typename T> inline Source<T> source_of(const Mat& m, long long row, long long rows, long long cols) {
+  Source<T> s{row_of<const T>(m, row), m.ld, nullptr};
+  if (s.p) s.end = s.p + (rows - 1) * m.ld + cols;
+  return s;
+}
+
 }  // namespace fa

@@ -116,8 +116,7 @@ __device__ __forceinline__ float mean_of(float sum, const Shape& s) {
 
 template <typename T>
 struct Forward {
-  const T* x; long long ldx;
-  const T* residual; long long ldr;
+  Source<T> x, residual;              // residual.p may be null
   ParamVec weight, bias;
   float eps;
   T* y; long long ldy;
@@ -143,19 +142,19 @@ __global__ void __launch_bounds__(kForwardThreads<K>, 1) forward_kernel(Forward<
   const int turns = static_cast<int>((s.rows + stride - 1) / stride);   // the same for every thread: all take part in the sums
   long long r = (long long)blockIdx.x * teams + mine;
   const int first = t * 8, apart_by = s.team * 8;               // chunk k starts at first + k * apart_by
-  const T* xp = a.x + r * a.ldx;
-  const T* up = a.residual ? a.residual + r * a.ldr : nullptr;
+  const T* xp = a.x.p + r * a.x.ld;
+  const T* up = a.residual.p ? a.residual.p + r * a.residual.ld : nullptr;
   T* yp = a.y + r * a.ldy;
   T* sp = a.sum_out ? a.sum_out + r * a.lds : nullptr;
   long long code = r * s.width + first, scale = r * s.scale_pitch + (first >> 5);
   const int pad = (first & 31) == 0 ? -s.groups & 3 : 0;
-  Raw8<T> x[K], u[K];
+  Chunk<T, VEC> x[K], u[K];
   auto load = [&](bool live) {
     const int cols = live ? s.cols : 0;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      x[k] = load_chunk<T, VEC>(xp, first + k * apart_by, cols);
-      if (up) u[k] = load_chunk<T, VEC>(up, first + k * apart_by, cols);
+      x[k].fetch(a.x, xp, first + k * apart_by, cols);
+      if (up) u[k].fetch(a.residual, up, first + k * apart_by, cols);
     }
   };
   load(r < s.rows);
@@ -164,18 +163,19 @@ __global__ void __launch_bounds__(kForwardThreads<K>, 1) forward_kernel(Forward<
     F2 v[K][4], part = two(0.f);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      x[k].get(v[k]);
+      const bool in = first + k * apart_by < s.cols;
+      x[k].raw(in).get(v[k]);
       if (up) {
         F2 w[4];
-        u[k].get(w);
+        u[k].raw(in).get(w);
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[k][j] = add2(v[k][j], w[j]);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) part = add2(part, v[k][j]);
     }
-    xp += stride * a.ldx;
-    if (up) up += stride * a.ldr;
+    xp += stride * a.x.ld;
+    if (up) up += stride * a.residual.ld;
     load(r + stride < s.rows);
     float sum[1] = {sum_of(part)};
     team_sum(sum, s.team, buf, &phase);
@@ -255,10 +255,13 @@ __global__ void __launch_bounds__(kBlock) forward_long_kernel(Forward<T> a, Shap
   const int turns = (s.width / 8 + kBlock - 1) / kBlock, lane = threadIdx.x & 31;
   for (long long r = blockIdx.x; r < s.rows; r += gridDim.x) {
     auto value = [&](int first, float (&v)[8]) {
-      load_chunk<T, VEC>(a.x + r * a.ldx, first, s.cols).get(v);
-      if (a.residual) {
+      Chunk<T, VEC> in;
+      in.fetch(a.x, a.x.p + r * a.x.ld, first, s.cols);
+      in.raw(first < s.cols).get(v);
+      if (a.residual.p) {
         float u[8];
-        load_chunk<T, VEC>(a.residual + r * a.ldr, first, s.cols).get(u);
+        in.fetch(a.residual, a.residual.p + r * a.residual.ld, first, s.cols);
+        in.raw(first < s.cols).get(u);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] += u[j];
       }
@@ -312,13 +315,12 @@ __global__ void __launch_bounds__(kBlock) forward_long_kernel(Forward<T> a, Shap
 
 template <typename T>
 struct Backward {
-  const T* dy; long long lddy;
-  const T* x; long long ldx;          // null: read the checkpoint
+  Source<T> dy, x;                    // x.p null: read the checkpoint
   Act8 ck;
   ParamVec weight;
   const float* mean;
   const float* rstd;
-  const T* residual; long long ldr;
+  Source<T> residual;
   T* dx; long long lddx;
   float* partials;                    // [gridDim.x][2][width], or null
 };
@@ -326,18 +328,18 @@ struct Backward {
 // The normalised input as it lies in memory: values, or a checkpoint's codes.
 template <typename T, bool VEC, bool CK>
 struct Input {
-  Raw8<T> x;
+  Chunk<T, VEC> x;
   // the first `cols` elements of row r exist
   __device__ __forceinline__ void load(const Backward<T>& a, const Shape&, long long r, int first, int cols) {
-    x = load_chunk<T, VEC>(a.x + r * a.ldx, first, cols);
+    x.fetch(a.x, a.x.p + r * a.x.ld, first, cols);
   }
-  template <typename V> __device__ __forceinline__ void get(V& v) const { x.get(v); }
+  __device__ __forceinline__ void get(F2 (&v)[4]) const { x.raw(true).get(v); }
 };
 template <typename T, bool VEC>
 struct Input<T, VEC, true> {
   RawAct8 x;
   __device__ __forceinline__ void load(const Backward<T>& a, const Shape& s, long long r, int first, int cols) {
-    x.load(a.ck.codes + r * s.width + first, a.ck.scales + r * s.scale_pitch + (first >> 5), first < cols);
+    x.load(a.ck, r * s.width + first, r * s.scale_pitch + (first >> 5), first < cols);
   }
   __device__ __forceinline__ void get(F2 (&v)[4]) const { x.get(v); }
 };
@@ -395,19 +397,18 @@ __global__ void __launch_bounds__((kBackwardThreads<T, K>), 1) backward_kernel(B
   const int turns = static_cast<int>((s.rows + stride - 1) / stride);
   long long r = (long long)blockIdx.x * teams + mine;
   const int first = t * 8, apart_by = s.team * 8;
-  const T* dyp = a.dy + r * a.lddy;
-  const T* xp = CK ? nullptr : a.x + r * a.ldx;
-  const uint8_t* codes = CK ? a.ck.codes + r * s.width + first : nullptr;
-  const uint8_t* scales = CK ? a.ck.scales + r * s.scale_pitch + (first >> 5) : nullptr;
-  const T* up = a.residual ? a.residual + r * a.ldr : nullptr;
+  const T* dyp = a.dy.p + r * a.dy.ld;
+  const T* xp = CK ? nullptr : a.x.p + r * a.x.ld;
+  long long code = r * s.width + first, scale = r * s.scale_pitch + (first >> 5);
+  const T* up = a.residual.p ? a.residual.p + r * a.residual.ld : nullptr;
   T* dxp = a.dx + r * a.lddx;
   F2 dw[K][4], db[K][4];
 #pragma unroll
   for (int k = 0; k < K; ++k)
 #pragma unroll
     for (int j = 0; j < 4; ++j) dw[k][j] = db[k][j] = two(0.f);
-  constexpr bool kResidualAhead = sizeof(T) == 2 || K == 1;        // (more fp32 rows ahead would not fit the registers)
-  Raw8<T> in_dy[K], in_x[CK ? 1 : K], in_u[K], next_u[K];
+  constexpr bool kResidualAhead = VEC && (sizeof(T) == 2 || K == 1);        // (elsewhere it would not fit the registers)
+  Chunk<T, VEC> in_dy[K], in_x[CK ? 1 : K], in_u[K], next_u[K];
   RawAct8 in_q[CK ? K : 1];
   float mean = 0.f, rstd = 0.f;
   auto load = [&](long long row) {
@@ -418,10 +419,10 @@ __global__ void __launch_bounds__((kBackwardThreads<T, K>), 1) backward_kernel(B
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int at = first + k * apart_by;
-      in_dy[k] = load_chunk<T, VEC>(dyp, at, cols);
-      if constexpr (CK) in_q[k].load(codes + k * apart_by, scales + k * (apart_by >> 5), at < cols);
-      else in_x[k] = load_chunk<T, VEC>(xp, at, cols);
-      if (kResidualAhead && up) next_u[k] = load_chunk<T, VEC>(up, at, cols);
+      in_dy[k].fetch(a.dy, dyp, at, cols);
+      if constexpr (CK) in_q[k].load(a.ck, code + k * apart_by, scale + k * (apart_by >> 5), at < cols);
+      else in_x[k].fetch(a.x, xp, at, cols);
+      if (kResidualAhead && up) next_u[k].fetch(a.residual, up, at, cols);
     }
   };
   load(r);
@@ -430,7 +431,7 @@ __global__ void __launch_bounds__((kBackwardThreads<T, K>), 1) backward_kernel(B
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       if (kResidualAhead) in_u[k] = next_u[k];
-      else if (up) in_u[k] = load_chunk<T, VEC>(up, first + k * apart_by, live ? s.cols : 0);
+      else if (up) in_u[k].fetch(a.residual, up, first + k * apart_by, live ? s.cols : 0);
     }
     const F2 rstd2 = two(rstd), minus_mean = two(-mean);
     F2 g[K][4], h[K][4], sg = two(0.f), sgh = two(0.f);
@@ -444,9 +445,9 @@ __global__ void __launch_bounds__((kBackwardThreads<T, K>), 1) backward_kernel(B
       }
       F2 w[4], dy[4];
       weight.get((first + k * apart_by) >> 3, w);
-      in_dy[k].get(dy);
+      in_dy[k].raw(true).get(dy);
       if constexpr (CK) in_q[k].get(h[k]);
-      else in_x[k].get(h[k]);
+      else in_x[k].raw(true).get(h[k]);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         // (past the row's end dy is zero, and h only ever meets it or is not stored)
@@ -458,14 +459,14 @@ __global__ void __launch_bounds__((kBackwardThreads<T, K>), 1) backward_kernel(B
         db[k][j] = add2(db[k][j], dy[j]);
       }
     }
-    dyp += stride * a.lddy;
+    dyp += stride * a.dy.ld;
     if constexpr (CK) {
-      codes += stride * s.width;
-      scales += stride * s.scale_pitch;
+      code += stride * s.width;
+      scale += stride * s.scale_pitch;
     } else {
-      xp += stride * a.ldx;
+      xp += stride * a.x.ld;
     }
-    if (up) up += stride * a.ldr;
+    if (up) up += stride * a.residual.ld;
     load(r + stride);
     float sum[2] = {sum_of(sg), sum_of(sgh)};
     team_sum(sum, s.team, buf, &phase);
@@ -474,9 +475,9 @@ __global__ void __launch_bounds__((kBackwardThreads<T, K>), 1) backward_kernel(B
     for (int k = 0; k < K; ++k) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) g[k][j] = mul2(fma2(h[k][j], mgh, add2(g[k][j], mg)), rstd2);
-      if (a.residual) {
+      if (up) {
         F2 u[4];
-        in_u[k].get(u);
+        in_u[k].raw(true).get(u);
 #pragma unroll
         for (int j = 0; j < 4; ++j) g[k][j] = add2(g[k][j], u[j]);
       }
@@ -506,7 +507,9 @@ __global__ void __launch_bounds__(kBlock) backward_stats_kernel(Backward<T> a, S
       F2 v2[4];
       float dy[8], v[8], w[8];
       in.load(a, s, r, first, s.cols);
-      load_chunk<T, VEC>(a.dy + r * a.lddy, first, s.cols).get(dy);
+      Chunk<T, VEC> in_dy;
+      in_dy.fetch(a.dy, a.dy.p + r * a.dy.ld, first, s.cols);
+      in_dy.raw(first < s.cols).get(dy);
       in.get(v2);
       load_param(a.weight, first, s.cols, 1.f, w);
 #pragma unroll
@@ -542,7 +545,9 @@ __global__ void __launch_bounds__(256) backward_long_kernel(Backward<T> a, Shape
     F2 v2[4];
     float dy[8], v[8], o[8];
     in.load(a, s, r, first, s.cols);
-    load_chunk<T, VEC>(a.dy + r * a.lddy, first, s.cols).get(dy);
+    Chunk<T, VEC> other;
+    other.fetch(a.dy, a.dy.p + r * a.dy.ld, first, s.cols);
+    other.raw(first < s.cols).get(dy);
     in.get(v2);
 #pragma unroll
     for (int j = 0; j < 4; ++j) apart(v2[j], &v[2 * j], &v[2 * j + 1]);
@@ -553,8 +558,9 @@ __global__ void __launch_bounds__(256) backward_long_kernel(Backward<T> a, Shape
       dw[j] = fmaf(dy[j], h, dw[j]);
       db[j] += dy[j];
     }
-    if (a.residual) {
-      load_chunk<T, VEC>(a.residual + r * a.ldr, first, s.cols).get(v);
+    if (a.residual.p) {
+      other.fetch(a.residual, a.residual.p + r * a.residual.ld, first, s.cols);
+      other.raw(first < s.cols).get(v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) o[j] += v[j];
     }
@@ -629,7 +635,7 @@ template <typename T, bool VEC>
 cudaError_t ln_forward_t(const ln::Forward<T>& a, long long rows, long long cols, cudaStream_t st) {
   ln::Shape s = ln_shape(rows, cols);
   int K = 1;
-  const int few = sizeof(T) == 2 ? 4 : 1, many = sizeof(T) == 2 ? 4 : 2;
+  const int few = sizeof(T) == 4 ? 1 : VEC ? 4 : 2, many = sizeof(T) == 2 && VEC ? 4 : 2;
   if (!ln_team(&s, VEC, few, many, ln::kMaxKForward, &K)) {
     const unsigned grid = static_cast<unsigned>(rows < (1 << 30) ? rows : 1 << 30);
     ln::forward_long_kernel<T, VEC><<<grid, ln::kBlock, 0, st>>>(a, s);
@@ -655,8 +661,8 @@ cudaError_t ln_forward_d(Mat x, Mat residual, long long rows, long long cols, Pa
                          Mat y, Mat sum_out, float* mean, float* rstd, void* ck_sum, void* ck_y, cudaStream_t st) {
   if (rows == 0) return cudaSuccess;
   ln::Forward<T> a{};
-  a.x = row_of<T>(x, 0); a.ldx = x.ld;
-  a.residual = row_of<T>(residual, 0); a.ldr = residual.ld;
+  a.x = source_of<T>(x, 0, rows, cols);
+  a.residual = source_of<T>(residual, 0, rows, cols);
   a.weight = param_vec(weight); a.bias = param_vec(bias);
   a.eps = eps;
   a.y = row_of<T>(y, 0); a.ldy = y.ld;
@@ -723,12 +729,12 @@ cudaError_t ln_backward_d(Mat dy, Mat x, const void* ck, long long rows, long lo
   const bool sums = dweight || dbias;
   if (rows > 0) {
     ln::Backward<T> a{};
-    a.dy = row_of<T>(dy, 0); a.lddy = dy.ld;
-    a.x = row_of<T>(x, 0); a.ldx = x.ld;
+    a.dy = source_of<T>(dy, 0, rows, cols);
+    a.x = source_of<T>(x, 0, rows, cols);
     a.ck = act8_at(ck, rows, cols, 0);
     a.weight = param_vec(weight);
     a.mean = mean; a.rstd = rstd;
-    a.residual = row_of<T>(residual, 0); a.ldr = residual.ld;
+    a.residual = source_of<T>(residual, 0, rows, cols);
     a.dx = row_of<T>(dx, 0); a.lddx = dx.ld;
     a.partials = sums ? partials : nullptr;
     const cudaError_t e = ck ? (vec ? ln_backward_t<T, true, true>(a, g, row_stats, st)

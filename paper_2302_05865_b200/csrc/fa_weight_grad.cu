@@ -588,7 +588,7 @@ __global__ void __launch_bounds__(256) finish_kernel(Finish f) {
 // dY as bf16 terms that add up to it exactly, rows of `pitch` elements: [planes][rows][pitch].  Terms are
 // cut off rather than rounded, so that no finite value becomes infinite; what is not finite is one term.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ dy, long long ld, long long rows, int outs,
+__global__ void __launch_bounds__(256) pack_kernel(Source<T> dy, long long rows, int outs,
                                                    int pitch, int planes, bf16* __restrict__ out) {
   const int per_row = pitch / 8;
   const long long n = rows * per_row, plane = rows * pitch;
@@ -596,7 +596,9 @@ __global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ dy, lon
     const long long r = j / per_row;
     const int first = static_cast<int>(j - r * per_row) * 8;
     float v[8];
-    load_chunk<T, VEC>(dy + r * ld, first, outs).get(v);
+    Chunk<T, VEC> in;
+    in.fetch(dy, dy.p + r * dy.ld, first, outs);
+    in.raw(first < outs).get(v);
     for (int q = 0; q < planes; ++q) {
       float term[8];
 #pragma unroll
@@ -692,12 +694,12 @@ cudaError_t launch_linear_weight_grad(Mat dy, int dtype, long long rows, long lo
     const bool vec = dtype == FA_F32 && mat_vec<float>(dy, outs);
     const long long want = (rows * (p.pitch / 8) + 255) / 256, most = 16LL * sm_count();
     const unsigned grid = static_cast<unsigned>(want < most ? want : most);
-    auto go = [&](auto kernel, auto* src) {
-      kernel<<<grid, 256, 0, st>>>(src, dy.ld, rows, (int)outs, p.pitch, p.planes, packed);
+    auto go = [&](auto kernel, auto src) {
+      kernel<<<grid, 256, 0, st>>>(src, rows, (int)outs, p.pitch, p.planes, packed);
     };
-    if (dtype == FA_BF16) go(wgrad::pack_kernel<bf16, false>, row_of<const bf16>(dy, 0));
-    else if (vec) go(wgrad::pack_kernel<float, true>, row_of<const float>(dy, 0));
-    else go(wgrad::pack_kernel<float, false>, row_of<const float>(dy, 0));
+    if (dtype == FA_BF16) go(wgrad::pack_kernel<bf16, false>, source_of<bf16>(dy, 0, rows, outs));
+    else if (vec) go(wgrad::pack_kernel<float, true>, source_of<float>(dy, 0, rows, outs));
+    else go(wgrad::pack_kernel<float, false>, source_of<float>(dy, 0, rows, outs));
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     base = packed;
