@@ -209,6 +209,7 @@ struct Chunk {
     return v;
   }
 };
+static __device__ const uint4 kZeroBlocks[3] = {};     // read where there is nothing to read
 template <typename T>
 struct Chunk<T, false> {
   static constexpr int kOut = 8 * sizeof(T) / 4, kPer = 16 / sizeof(T);     // words of a chunk, elements of a block
@@ -221,15 +222,12 @@ struct Chunk<T, false> {
     valid = cols - first;
     const T* a = p - (static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) & 15u) / sizeof(T);
     whole = valid > 0 && a >= m.p && a + 8 + kPer <= m.end;
+    const uint4* b = whole ? reinterpret_cast<const uint4*>(a) : kZeroBlocks;
 #pragma unroll
-    for (int i = 0; i < kOut + 4; ++i) w[i] = 0;
-    const uint4* b = reinterpret_cast<const uint4*>(a);
-#pragma unroll
-    for (int i = 0; i < kOut / 4 + 1; ++i)
-      if (whole) {
-        const uint4 t = b[i];
-        w[4 * i] = t.x; w[4 * i + 1] = t.y; w[4 * i + 2] = t.z; w[4 * i + 3] = t.w;
-      }
+    for (int i = 0; i < kOut / 4 + 1; ++i) {
+      const uint4 t = b[i];
+      w[4 * i] = t.x; w[4 * i + 1] = t.y; w[4 * i + 2] = t.z; w[4 * i + 3] = t.w;
+    }
   }
   __device__ __forceinline__ Raw8<T> raw(bool) const {
     Raw8<T> r;
