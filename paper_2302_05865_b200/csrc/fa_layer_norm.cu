@@ -99,11 +99,12 @@ __device__ __forceinline__ ParamCache cache_param(float* room, const ParamVec& w
   ParamCache c;
   c.half[0] = reinterpret_cast<float4*>(room);
   c.half[1] = c.half[0] + chunks;
-  for (int i = threadIdx.x; i < s.width; i += blockDim.x) {
-    float v = 0.f;
-    if (i < s.cols)
-      v = !w.p ? none : w.is_bf16 ? to_float(static_cast<const bf16*>(w.p)[i]) : static_cast<const float*>(w.p)[i];
-    room[((i & 4) ? chunks * 4 : 0) + (i >> 3) * 4 + (i & 3)] = v;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < chunks; i += blockDim.x) {
+    float v[8];
+    load_param(w, i * 8, s.cols, none, v);
+    c.half[0][i] = make_float4(v[0], v[1], v[2], v[3]);
+    c.half[1][i] = make_float4(v[4], v[5], v[6], v[7]);
   }
   return c;
 }
@@ -132,9 +133,7 @@ template <typename T, bool VEC, int K>
 __global__ void __launch_bounds__(kForwardThreads<K>, 1) forward_kernel(Forward<T> a, Shape s) {
   extern __shared__ float4 dyn4[];          // weight and bias
   float* room = reinterpret_cast<float*>(dyn4);
-  const ParamCache weight = cache_param(room, a.weight, s, 1.f), bias = cache_param(room + s.width, a.bias, s, 0.f);
   __shared__ TeamSums<1> buf;
-  clear_sums(buf);
   int phase = 0;
   const int teams = blockDim.x / s.team, t = threadIdx.x % s.team, mine = threadIdx.x / s.team, lane = threadIdx.x & 31;
   const bool prev = lane > 0 && t > 0, next = lane < 31 && t + 1 < s.team;      // neighbours of the same row
@@ -158,6 +157,8 @@ __global__ void __launch_bounds__(kForwardThreads<K>, 1) forward_kernel(Forward<
     }
   };
   load(r < s.rows);
+  const ParamCache weight = cache_param(room, a.weight, s, 1.f), bias = cache_param(room + s.width, a.bias, s, 0.f);
+  clear_sums(buf);
   for (int i = 0; i < turns; ++i) {
     const bool live = r < s.rows;
     F2 v[K][4], part = two(0.f);
@@ -387,9 +388,7 @@ template <typename T, bool VEC, int K, bool CK>
 __global__ void __launch_bounds__((kBackwardThreads<T, K>), 1) backward_kernel(Backward<T> a, Shape s) {
   extern __shared__ float4 dyn4[];          // the weight; then the column sums of the block's other teams
   float* dyn = reinterpret_cast<float*>(dyn4) + s.width;
-  const ParamCache weight = cache_param(reinterpret_cast<float*>(dyn4), a.weight, s, 1.f);
   __shared__ TeamSums<2> buf;
-  clear_sums(buf);
   int phase = 0;
   const int teams = blockDim.x / s.team, t = threadIdx.x % s.team, mine = threadIdx.x / s.team, lane = threadIdx.x & 31;
   const bool prev = lane > 0 && t > 0, next = lane < 31 && t + 1 < s.team;
@@ -426,6 +425,8 @@ __global__ void __launch_bounds__((kBackwardThreads<T, K>), 1) backward_kernel(B
     }
   };
   load(r);
+  const ParamCache weight = cache_param(reinterpret_cast<float*>(dyn4), a.weight, s, 1.f);
+  clear_sums(buf);
   for (int i = 0; i < turns; ++i) {
     const bool live = r < s.rows;
 #pragma unroll
@@ -607,7 +608,8 @@ ln::Shape ln_shape(long long rows, long long cols) {
 bool ln_team(ln::Shape* s, bool vec, int few, int many, int max_k, int* K) {
   const int chunks = s->width / 8;
   if (chunks > ln::kBlock * max_k) return false;
-  *K = chunks <= 256 ? few : many;
+  // up to one row per SM there is only the one row's latency to shorten: as many threads as it has chunks
+  *K = s->rows <= sm_count() ? 1 : chunks <= 256 ? few : many;
   while (*K * ln::kBlock < chunks) *K *= 2;
   while (*K > 1 && chunks <= 32 * (*K / 2)) *K /= 2;
   auto places = [&](int k) { return ((chunks + k - 1) / k + 31) / 32 * 32 * k; };

@@ -89,32 +89,38 @@ def _matrix(t, name):
     return t.data_ptr(), ld, t.numel() // cols, cols, code, t.device
 
 
+def _where(t, name, device):
+    return ValueError(f"{name} must be a CUDA tensor" if not t.is_cuda else f"{name} is on {t.device}, the call runs on {device}")
+
+
 def _like(t, name, rows, cols, dtype, device):
     """(pointer, row stride) of another activation of the same call."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
-    if t.dtype != dtype or t.numel() != rows * cols or not t.dim() or t.shape[-1] != cols:
-        raise ValueError(f"{name} must have {rows} rows of {cols} elements of {dtype}, got {tuple(t.shape)} of {t.dtype}")
+    shape = t.shape
+    if t.dtype is not dtype or not shape or shape[-1] != cols or t.numel() != rows * cols:
+        raise ValueError(f"{name} must have {rows} rows of {cols} elements of {dtype}, got {tuple(shape)} of {t.dtype}")
     ld = cols if t.is_contiguous() else _row_stride(t, name)
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, the call runs on {device}")
+    if t.get_device() != device.index:
+        raise _where(t, name, device)
     return t.data_ptr(), ld
 
 
 def _vector(t, numel, name, device, dtype=None):
     """Pointer of a contiguous tensor of exactly `numel` elements, of `dtype` or of either float type."""
-    if dtype is None:
-        _code(t, name)
-    elif not isinstance(t, torch.Tensor):
+    if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
-    elif t.dtype != dtype:
+    if dtype is None:
+        if t.dtype not in _CODES:
+            raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+    elif t.dtype is not dtype:
         raise ValueError(f"{name} must have dtype {dtype}, got {t.dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     if t.numel() != numel:
         raise ValueError(f"{name} must have {numel} elements, got {t.numel()}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, the call runs on {device}")
+    if t.get_device() != device.index:
+        raise _where(t, name, device)
     return t.data_ptr()
 
 
@@ -129,17 +135,15 @@ def _buffer(t, nbytes, name, device):
         raise TypeError(f"{name} must be a torch tensor")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if t.numel() * t.element_size() < nbytes:
-        raise ValueError(f"{name} must have at least {nbytes} bytes, got {t.numel() * t.element_size()}")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, the call runs on {device}")
+    if t.nbytes < nbytes:
+        raise ValueError(f"{name} must have at least {nbytes} bytes, got {t.nbytes}")
+    if not t.is_cuda or t.get_device() != device.index:
+        raise _where(t, name, device)
     return t.data_ptr()
 
 
 def _opt_checkpoint(t, rows, cols, name, device):
-    return None if t is None else _buffer(t, fa_checkpoint8_bytes(rows, cols), name, device)
+    return None if t is None else _buffer(t, _bytes_of("fa_checkpoint8_bytes", rows, cols), name, device)
 
 
 def _grad(t, shape, numel, name, device, partner=None):
@@ -187,7 +191,7 @@ def _workspace(ws, nbytes, device):
     if ws is None:
         ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
         return ws, ws.data_ptr(), nbytes
-    return ws, _buffer(ws, nbytes, "ws", device), ws.numel() * ws.element_size()
+    return ws, _buffer(ws, nbytes, "ws", device), ws.nbytes
 
 
 def _approximate(name):
@@ -258,20 +262,25 @@ def fa_layer_norm_forward(x, weight=None, bias=None, eps=1e-5, residual=None, y=
     elif bp is not None and bcode != pcode:
         raise ValueError("weight and bias must have the same dtype")
     with _on(dev, stream):
-        yp, ldy = _like(y, "y", rows, cols, dtype, dev) if y is not None else (None, cols)
         if y is None:
             y = _fresh(x)
-            yp = y.data_ptr()
+            yp, ldy = y.data_ptr(), cols
+        else:
+            yp, ldy = _like(y, "y", rows, cols, dtype, dev)
+        sp, lds = (None, 0) if sum_out is None else _like(sum_out, "sum_out", rows, cols, dtype, dev)
         if sum_out is None and residual is not None:
             sum_out = _fresh(x)
-        sp, lds = (None, 0) if sum_out is None else _like(sum_out, "sum_out", rows, cols, dtype, dev)
+            sp, lds = sum_out.data_ptr(), cols
         if mean is None:
             mean = torch.empty(rows, dtype=torch.float32, device=dev)
+        else:
+            _vector(mean, rows, "mean", dev, torch.float32)
         if rstd is None:
             rstd = torch.empty(rows, dtype=torch.float32, device=dev)
+        else:
+            _vector(rstd, rows, "rstd", dev, torch.float32)
         _check(_lib.fa_layer_norm_forward(
-            xp, ldx, rp, ldr, code, rows, cols, wp, bp, pcode, eps, yp, ldy, sp, lds,
-            _vector(mean, rows, "mean", dev, torch.float32), _vector(rstd, rows, "rstd", dev, torch.float32),
+            xp, ldx, rp, ldr, code, rows, cols, wp, bp, pcode, eps, yp, ldy, sp, lds, mean.data_ptr(), rstd.data_ptr(),
             _opt_checkpoint(ck_sum, rows, cols, "ck_sum", dev), _opt_checkpoint(ck_y, rows, cols, "ck_y", dev),
             _raw_stream(dev.index)), "fa_layer_norm_forward")
     return y, mean, rstd, x if sum_out is None else sum_out
