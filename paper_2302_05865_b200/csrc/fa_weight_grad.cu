@@ -48,10 +48,14 @@ constexpr int kColumnWarp = kScaleWarp + 1;
 template <bool SIDE> constexpr int kThreads = 32 * (kColumnWarp + (SIDE ? 4 : 0));
 
 // A tile of kIns * PAIR inputs x N outputs, by one block or by a pair of blocks on neighbouring SMs.  In a pair each
-// block holds its own 128 inputs and half of dY's columns, and the tensor cores read the other half from the
-// neighbour.  Shared memory moves 128 bytes a cycle for the copies, the converters and the products together: for
-// N = 256 a step costs 898 of its cycles with one block and 642 with a pair, and the products take 512.
+// block holds its own 128 inputs and half of every 256 of dY's columns, and the tensor cores read the other half from
+// the neighbour.  Shared memory moves 128 bytes a cycle for the copies, the converters and the products together: a
+// step of 256 outputs, whose products take 512 cycles, costs 898 of its cycles with one block, 642 with a pair and 513
+// with a pair whose tile has 512 outputs, where converted codes are used twice.  Such a tile fills tensor memory, so
+// that it cannot be read out while the next one is summed.
 template <int N, int PAIR> struct Cfg {
+  static constexpr int kMma = N < 256 ? N : 256;     // outputs of one instruction
+  static constexpr int kAccs = N == 512 ? 1 : 2;     // accumulators; one takes N of the 512 columns of tensor memory
   static constexpr int kBytesB = N / PAIR / 64 * kBoxBytes;
   static constexpr int kStage = kBytesA + kBytesB;   // a stage: codes as bf16, then dY
   static constexpr int kStages = N / PAIR == 256 ? 4 : 5;
@@ -60,7 +64,7 @@ template <int N, int PAIR> struct Cfg {
   static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + (size_t)kStagesRaw * kRawBytes + 256;
   // kind::f16: D fp32, A and B bf16, both MN-major, M = 128 or 256
   static constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) |
-                                     ((uint32_t)(N >> 3) << 17) | ((uint32_t)(kIns * PAIR >> 4) << 24);
+                                     ((uint32_t)(kMma >> 3) << 17) | ((uint32_t)(kIns * PAIR >> 4) << 24);
 };
 
 struct Params {
@@ -238,7 +242,7 @@ struct ColumnSums {
     const int halves = first < w.k1 ? 2 * ((w.k1 - first + p.tiles_i - 1) / p.tiles_i) : 0;
     float* out = p.columns + ((size_t)(w.split * p.tiles_i + tile_i) * 4 + warp) * p.width;
     for (int c = 0; c < kCols; c += 128) {
-      const int col = w.o0 + rank * kCols + c + (lane & 15) * 8;
+      const int col = w.o0 + (c >> 7) * (128 * PAIR) + rank * 128 + (lane & 15) * 8;
       F2 acc[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[i] = two(0.f);
@@ -313,12 +317,12 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
   if (warp == 1) {
     if constexpr (PAIR == 1) {
       asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)),
-                   "r"(2 * N)
+                   "r"(C::kAccs * N)
                    : "memory");
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     } else {
       asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)),
-                   "r"(2 * N)
+                   "r"(C::kAccs * N)
                    : "memory");
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
@@ -346,7 +350,8 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
           unsigned char* b = stages + (size_t)s * C::kStage + kBytesA;
 #pragma unroll
           for (int q = 0; q < N / PAIR / 64; ++q)
-            tma_load_3d<PAIR>(b + q * kBoxBytes, &map_dy, w.o0 + rank * (N / PAIR) + q * 64, k * kTokens, pl, &bars->full[s]);
+            tma_load_3d<PAIR>(b + q * kBoxBytes, &map_dy, w.o0 + (q >> 1) * (128 * PAIR) + rank * 128 + (q & 1) * 64, k * kTokens, pl,
+                              &bars->full[s]);
           if (++pl == prm.planes) { pl = 0; ++k; }
         }
       }
@@ -365,8 +370,8 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
         const Unit w = unit_of<N, PAIR>(prm, u, rank);
         for (int j0 = w.k0; j0 < w.k1 && ok; j0 += prm.run, ++nu) {
           const int j1 = min(j0 + prm.run, w.k1);
-          const uint32_t acc = nu & 1, d = tmem_base + acc * N;
-          ok = mbar_wait(&bars->acc_empty[acc], ((nu >> 1) & 1) ^ 1);
+          const uint32_t acc = nu % C::kAccs, d = tmem_base + acc * N;
+          ok = mbar_wait(&bars->acc_empty[acc], ((nu / C::kAccs) & 1) ^ 1);
           for (int j = j0; j < j1 && ok; ++j, ++n) {
             const int s = n % C::kStages;
             ok = mbar_wait(&bars->full[s], (n / C::kStages) & 1);
@@ -375,7 +380,10 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
             const uint32_t a = smem_u32(stages + (size_t)s * C::kStage), b = a + kBytesA;
 #pragma unroll
             for (int q = 0; q < kTokens / 16; ++q)      // 16 tokens are two groups of 8: 2048 bytes
-              umma<PAIR>(d, mn_desc(a + q * 2048), mn_desc(b + q * 2048), C::kIdesc, (j == j0 && q == 0) ? 0u : 1u);
+#pragma unroll
+              for (int h = 0; h < N / C::kMma; ++h)
+                umma<PAIR>(d + h * C::kMma, mn_desc(a + q * 2048), mn_desc(b + h * (C::kMma / PAIR / 64) * kBoxBytes + q * 2048),
+                           C::kIdesc, (j == j0 && q == 0) ? 0u : 1u);
             umma_commit<PAIR>(&bars->empty[s]);
           }
           if (ok) umma_commit<PAIR>(&bars->acc_full[acc]);
@@ -405,8 +413,8 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
       if (!SIDE && prm.columns)
         ColumnSums<N, PAIR>::run(prm, w, (u - w.split * prm.tiles) % prm.tiles_i, rank, warp & 3, lane);
       for (int j0 = w.k0; j0 < w.k1; j0 += prm.run, ++nu) {
-        const uint32_t acc = nu & 1;
-        ok = __all_sync(0xffffffffu, ok && mbar_wait(&bars->acc_full[acc], (nu >> 1) & 1));
+        const uint32_t acc = nu % C::kAccs;
+        ok = __all_sync(0xffffffffu, ok && mbar_wait(&bars->acc_full[acc], (nu / C::kAccs) & 1));
         tc_fence_after();
         for (int c = 0; c < N; c += 32) {
           uint32_t v[32];
@@ -535,9 +543,9 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
   if (warp == 1) {
     tc_fence_after();
     if constexpr (PAIR == 1)
-      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(2 * N) : "memory");
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(C::kAccs * N) : "memory");
     else
-      asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(2 * N) : "memory");
+      asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(C::kAccs * N) : "memory");
   }
 }
 
@@ -614,6 +622,8 @@ __global__ void __launch_bounds__(256) pack_kernel(Source<T> dy, long long rows,
   }
 }
 
+constexpr double kWideStep = 1.55;       // time of a step with 512 outputs, in steps with 256 (0.74 and 0.48 us)
+
 // How a product is cut up.  Per block and stage the MMA takes N / 256 * 512 cycles or so; a split costs
 // a write and a read of the whole result.
 struct Plan {
@@ -623,29 +633,39 @@ struct Plan {
   size_t pack_bytes, split_stride, partial_bytes, column_bytes;
 };
 
-Plan plan_of(long long rows, long long outs, long long ins, int dtype, bool pack) {
+// `gdtype` of the result: one in fp32 is read out in runs, which a tile of 512 outputs would have to wait for.
+Plan plan_of(long long rows, long long outs, long long ins, int dtype, int gdtype, bool pack) {
   Plan p{};
   p.planes = dtype == FA_F32 ? 3 : 1;
   p.pack = pack;
   p.pitch = static_cast<int>((outs + 7) / 8 * 8);
   p.pack_bytes = pack ? ((size_t)p.planes * rows * p.pitch * 2 + 255) / 256 * 256 : 0;
+  p.ksteps = static_cast<int>((rows + kTokens - 1) / kTokens) * p.planes;
+  auto cut = [&](int n, int pair, double step) {
+    p.n = n;
+    p.pair = pair;
+    p.tiles_i = static_cast<int>((ins + kIns * pair - 1) / (kIns * pair));
+    p.tiles_o = static_cast<int>((outs + n - 1) / n);
+    const long long tiles = (long long)p.tiles_i * p.tiles_o, blocks = sm_count() / pair;
+    p.tiles = static_cast<int>(tiles);
+    // splits that fill the blocks once; each keeps at least 4 stages
+    long long s = tiles >= blocks ? 1 : blocks / tiles;
+    if (s > (p.ksteps + 3) / 4) s = (p.ksteps + 3) / 4;
+    if (s > 32) s = 32;
+    p.splits = static_cast<int>(s < 1 ? 1 : s);
+    // time of the busiest block in steps with 256 outputs (0.47 us), and what writing, reading and adding the splits
+    // costs in these (2 TB/s: little of it is hidden)
+    const long long turns = (tiles * p.splits + blocks - 1) / blocks;
+    return (double)turns * ((p.ksteps + p.splits - 1) / p.splits) * step +
+           (p.splits > 1 ? (double)p.splits * outs * ins * 8.0 / 2e6 / 0.47 : 0.0);
+  };
   // Tiles of 128 x 128 by single blocks where there is little to do: more blocks share the read-out, and no pair has to
   // be set up (256 x 256 from 512 tokens 8.8 against 12.5 us, 768 x 768 from 2048 14.8 against 15.8); pairs for more
   // (1024 x 1024 from 8192 29.9 against 41.3).
   const bool little = (double)rows * (double)outs * (double)ins * p.planes <= 2147483648.0;
-  p.n = little || outs <= 128 ? 128 : 256;
-  p.pair = !little && ins > kIns && outs > 128 ? 2 : 1;
-  p.tiles_i = static_cast<int>((ins + kIns * p.pair - 1) / (kIns * p.pair));
-  p.tiles_o = static_cast<int>((outs + p.n - 1) / p.n);
-  p.ksteps = static_cast<int>((rows + kTokens - 1) / kTokens) * p.planes;
-  const long long tiles = (long long)p.tiles_i * p.tiles_o;
-  p.tiles = static_cast<int>(tiles);
-  const int sms = sm_count() / p.pair;
-  // splits that fill the blocks once; each keeps at least 4 stages
-  long long s = tiles >= sms ? 1 : sms / tiles;
-  if (s > (p.ksteps + 3) / 4) s = (p.ksteps + 3) / 4;
-  if (s > 32) s = 32;
-  p.splits = static_cast<int>(s < 1 ? 1 : s);
+  const int n = little || outs <= 128 ? 128 : 256, pair = !little && ins > kIns && outs > 128 ? 2 : 1;
+  const double cost = cut(n, pair, 1.0);
+  if (pair == 2 && outs > 256 && gdtype == FA_BF16 && cut(512, 2, kWideStep) >= cost) cut(n, pair, 1.0);
   p.split_stride = ((size_t)outs * ins + 63) / 64 * 64;
   p.partial_bytes = p.splits > 1 ? p.splits * p.split_stride * sizeof(float) : 0;
   p.column_bytes = (size_t)p.splits * p.tiles_i * 4 * p.pitch * sizeof(float);
@@ -655,8 +675,10 @@ Plan plan_of(long long rows, long long outs, long long ins, int dtype, bool pack
 }  // namespace wgrad
 
 size_t linear_weight_grad_scratch_bytes(long long rows, long long outs, long long ins, int dtype) {
-  const wgrad::Plan p = wgrad::plan_of(rows, outs, ins, dtype, true);   // whether dY has to be laid out is known at the call
-  return p.pack_bytes + p.partial_bytes + p.column_bytes;
+  // whether dY has to be laid out, and the type of the result, are known at the call
+  const wgrad::Plan p = wgrad::plan_of(rows, outs, ins, dtype, FA_F32, true), q = wgrad::plan_of(rows, outs, ins, dtype, FA_BF16, true);
+  const size_t a = p.partial_bytes + p.column_bytes, b = q.partial_bytes + q.column_bytes;
+  return p.pack_bytes + (a > b ? a : b);
 }
 
 template <int N, int PAIR, bool SIDE>
@@ -690,7 +712,7 @@ cudaError_t launch_linear_weight_grad(Mat dy, int dtype, long long rows, long lo
     return e != cudaSuccess || !dbias ? e : cudaMemsetAsync(dbias, 0, outs * g, st);
   }
   const bool direct = dtype == FA_BF16 && aligned16(dy.p) && dy.ld % 8 == 0 && dy.ld >= outs && dy.ld < (1LL << 38);
-  const wgrad::Plan p = wgrad::plan_of(rows, outs, ins, dtype, !direct);
+  const wgrad::Plan p = wgrad::plan_of(rows, outs, ins, dtype, gdtype, !direct);
   const void* base = dy.p;
   long long ld = dy.ld;
   if (!direct) {
@@ -749,7 +771,8 @@ cudaError_t launch_linear_weight_grad(Mat dy, int dtype, long long rows, long lo
   const bool side = dbias && (p.ksteps + p.splits - 1) / p.splits > prm.run;
   auto go = [&](auto with_side) {
     constexpr bool SIDE = decltype(with_side)::value;
-    return p.pair == 2  ? launch_product<256, 2, SIDE>(map, map_codes, prm, st)
+    return p.n == 512   ? launch_product<512, 2, SIDE>(map, map_codes, prm, st)
+           : p.pair == 2 ? launch_product<256, 2, SIDE>(map, map_codes, prm, st)
            : p.n == 256 ? launch_product<256, 1, SIDE>(map, map_codes, prm, st)
                         : launch_product<128, 1, SIDE>(map, map_codes, prm, st);
   };

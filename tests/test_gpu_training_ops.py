@@ -383,6 +383,31 @@ def test_linear_weight_grad(dtype, gdtype, rows, outs, ins, lead, gap):
     assert torch.isnan(row[:1]).all() and torch.isnan(row[1 + outs * (ins + 1):]).all()
 
 
+# more than 2^31 products: pairs of blocks and wider tiles; sums read out in several runs; narrow inputs
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("gdtype", TYPES)
+@pytest.mark.parametrize("rows,outs,ins", [(2100, 1030, 1100), (2300, 2310, 2330), (4200, 520, 1000), (33000, 300, 230),
+                                           (70000, 300, 120), (2304, 4096, 512), (40001, 640, 256)])
+def test_linear_weight_grad_of_many_products(dtype, gdtype, rows, outs, ins):
+    T, G = TYPES[dtype], TYPES[gdtype]
+    g = gen(rows + outs + ins)
+    dy = randn(g, rows, outs, dtype=T, scale=1e-2)
+    ck = fa().fa_checkpoint8_store(randn(g, rows, ins, dtype=T, scale=2.0) + 0.5)
+    x = ref.decode(ck, rows, ins).cuda()
+    row = torch.full((outs * (ins + 1) + 8,), math.nan, dtype=G, device="cuda")
+    dw, db = row[1:1 + outs * ins].view(outs, ins), row[1 + outs * ins:1 + outs * (ins + 1)]
+    fa().fa_linear_weight_grad(dy, ck, ins, dweight=dw, dbias=db)
+    exact, mags = dy.double().T @ x, dy.double().abs().T @ x.abs()
+    units = 2 * (rows / 16 + 34) + 16                            # as above
+    ref.assert_close(dw, exact, mags, units, "dweight")
+    if gdtype == "f32":      # summed in runs of 32 steps: 512 additions at two units, then at most rows / 2048 + 34 more
+        ref.assert_close(dw, exact, mags, 2 * (512 + rows / 512 + 34), "dweight in runs")
+    ref.assert_close(db, dy.double().sum(0), dy.double().abs().sum(0), rows / 8 + 128, "dbias")
+    assert torch.isnan(row[:1]).all() and torch.isnan(row[1 + outs * (ins + 1):]).all()
+    only, none = fa().fa_linear_weight_grad(dy, ck, ins, dweight=torch.empty(outs, ins, dtype=G, device="cuda"), dbias=False)
+    assert none is None and torch.equal(only, dw)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_linear_weight_grad_keeps_broken_values_in_their_places(dtype):
     rows, outs, ins = 70, 48, 200
