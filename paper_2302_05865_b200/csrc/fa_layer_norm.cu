@@ -4,8 +4,16 @@
 //             dw = column sums of dy h, db = column sums of dy
 // A team of threads holds a row in registers, `K` chunks of 8 values per thread, so the variance is formed from
 // centred values and nothing is read twice; the next row's loads are issued before the current row's sums, which
-// are what a row waits for.  A block has as many teams as fit into kBlock threads.  Rows of more than
-// kBlock * kMaxK chunks go through the `long` kernels, which read a row several times.
+// are what a row waits for.  One block per SM walks over the rows; the backward pass keeps its share of the column sums
+// in registers.  Rows that do not fit (more than 16384 columns forward, 8192 backward) go through the `long` kernels,
+// which read a row several times.
+// Memory is the floor; what holds the kernels above it is the number of instructions a row takes besides its values
+// (sums across lanes and warps, the scales of checkpoints): measured on bf16, 16384 rows of 4096,
+//   forward with residual, sum and two checkpoints 137 us (5.0 TB/s, 0.75 of a copy; 44 instructions a value, 62 % of
+//   the issue slots), backward from a checkpoint with residual gradient 108 + 5 us (4.3 TB/s, 0.64; 33 a value),
+// and of 768: 33 and 35 us (0.59, 0.39).  More chunks a thread spread those instructions over more values, fewer leave
+// registers for more warps: four (three) chunks are best in the forward pass (768 columns: 33 us, with one 41), one or
+// two, with two sums a column to keep, in the backward pass.
 #include "../../include/fa.h"
 #include "fa_columns.cuh"
 #include "fa_train.h"
