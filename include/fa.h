@@ -277,9 +277,12 @@ int fa_gelu_backward(const void* dy, long long lddy, const void* x, long long ld
 /* Gradient of a linear layer's weight and bias from the checkpoint of its input X (rows x ins):
  *   dweight[o][i] = sum over rows t of dy[t][o] * X[t][i]   (outs x ins, contiguous),
  *   dbias[o] = sum over rows t of dy[t][o]                  (NULL: not wanted).
- * rows <= FA_MAX_TOKENS, outs * ins <= 2^40.  Products are exact, sums fp32.  ws: fa_linear_weight_grad_workspace_bytes(). */
+ * rows <= FA_MAX_TOKENS, outs * ins <= 2^40.  Products are exact, sums fp32.  A device wait that runs out leaves NaN in
+ * the results it concerns.  ws: fa_linear_weight_grad_workspace_bytes(); aligned: non-zero if address and row stride of
+ * dy are multiples of 16 bytes (a bf16 dy is then read where it lies; any other is laid out in the workspace first). */
 #define FA_MAX_TOKENS 2147483520LL     /* 2^31 - 128 */
-int fa_linear_weight_grad_workspace_bytes(long long rows, long long outs, long long ins, int dtype, size_t* bytes);
+int fa_linear_weight_grad_workspace_bytes(long long rows, long long outs, long long ins, int dtype, int aligned,
+                                          size_t* bytes);
 int fa_linear_weight_grad(const void* dy, long long lddy, int dtype, long long rows, long long outs, const void* ck,
                           long long ins, void* dweight, void* dbias, int gdtype, void* ws, size_t ws_bytes,
                           void* stream);

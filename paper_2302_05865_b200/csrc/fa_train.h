@@ -46,6 +46,8 @@ cudaError_t launch_layer_norm_backward(Mat dy, Mat x, const void* ck, int dtype,
 
 cudaError_t launch_linear_weight_grad(Mat dy, int dtype, long long rows, long long outs, long long ins, const void* ck,
                                       void* dweight, void* dbias, int gdtype, void* scratch, cudaStream_t st);
-size_t linear_weight_grad_scratch_bytes(long long rows, long long outs, long long ins, int dtype);
+// whether dY is bf16 and TMA can address its rows
+bool linear_weight_grad_direct(Mat dy, int dtype, long long outs);
+size_t linear_weight_grad_scratch_bytes(long long rows, long long outs, long long ins, int dtype, bool direct);
 
 }  // namespace fa

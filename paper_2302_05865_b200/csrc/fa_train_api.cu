@@ -156,9 +156,10 @@ int fa_layer_norm_backward(const void* dy, long long lddy, const void* x, long l
       static_cast<cudaStream_t>(stream)));
 }
 
-int fa_linear_weight_grad_workspace_bytes(long long rows, long long outs, long long ins, int dtype, size_t* bytes) {
+int fa_linear_weight_grad_workspace_bytes(long long rows, long long outs, long long ins, int dtype, int aligned,
+                                          size_t* bytes) {
   if (!bytes || !fa::type_ok(dtype) || !fa::product_ok(rows, outs, ins)) return FA_ERR_ARG;
-  *bytes = fa::ws_round(fa::linear_weight_grad_scratch_bytes(rows, outs, ins, dtype));
+  *bytes = fa::ws_round(fa::linear_weight_grad_scratch_bytes(rows, outs, ins, dtype, aligned && dtype == FA_BF16));
   return FA_OK;
 }
 
@@ -171,7 +172,8 @@ int fa_linear_weight_grad(const void* dy, long long lddy, int dtype, long long r
   if (!fa::at(dy, fa::size_of(dtype)) || !fa::at(ck, 16) || !fa::at(dweight, fa::size_of(gdtype)) ||
       !fa::at(dbias, fa::size_of(gdtype)) || !fa::at(ws, 16))
     return FA_ERR_ALIGN;
-  if (ws_bytes < fa::linear_weight_grad_scratch_bytes(rows, outs, ins, dtype)) return FA_ERR_WORKSPACE;
+  const bool direct = fa::linear_weight_grad_direct({dy, lddy}, dtype, outs);
+  if (ws_bytes < fa::linear_weight_grad_scratch_bytes(rows, outs, ins, dtype, direct)) return FA_ERR_WORKSPACE;
   return fa::cuda_code(fa::launch_linear_weight_grad({dy, lddy}, dtype, rows, outs, ins, ck, dweight, dbias, gdtype, ws,
                                                      static_cast<cudaStream_t>(stream)));
 }

@@ -674,9 +674,14 @@ Plan plan_of(long long rows, long long outs, long long ins, int dtype, int gdtyp
 
 }  // namespace wgrad
 
-size_t linear_weight_grad_scratch_bytes(long long rows, long long outs, long long ins, int dtype) {
-  // whether dY has to be laid out, and the type of the result, are known at the call
-  const wgrad::Plan p = wgrad::plan_of(rows, outs, ins, dtype, FA_F32, true), q = wgrad::plan_of(rows, outs, ins, dtype, FA_BF16, true);
+bool linear_weight_grad_direct(Mat dy, int dtype, long long outs) {
+  return dtype == FA_BF16 && aligned16(dy.p) && dy.ld % 8 == 0 && dy.ld >= outs && dy.ld < (1LL << 38);
+}
+
+size_t linear_weight_grad_scratch_bytes(long long rows, long long outs, long long ins, int dtype, bool direct) {
+  // the type of the result is known at the call
+  const wgrad::Plan p = wgrad::plan_of(rows, outs, ins, dtype, FA_F32, !direct);
+  const wgrad::Plan q = wgrad::plan_of(rows, outs, ins, dtype, FA_BF16, !direct);
   const size_t a = p.partial_bytes + p.column_bytes, b = q.partial_bytes + q.column_bytes;
   return p.pack_bytes + (a > b ? a : b);
 }
@@ -711,7 +716,7 @@ cudaError_t launch_linear_weight_grad(Mat dy, int dtype, long long rows, long lo
     const cudaError_t e = cudaMemsetAsync(dweight, 0, n * g, st);
     return e != cudaSuccess || !dbias ? e : cudaMemsetAsync(dbias, 0, outs * g, st);
   }
-  const bool direct = dtype == FA_BF16 && aligned16(dy.p) && dy.ld % 8 == 0 && dy.ld >= outs && dy.ld < (1LL << 38);
+  const bool direct = linear_weight_grad_direct(dy, dtype, outs);
   const wgrad::Plan p = wgrad::plan_of(rows, outs, ins, dtype, gdtype, !direct);
   const void* base = dy.p;
   long long ld = dy.ld;

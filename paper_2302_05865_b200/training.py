@@ -35,7 +35,7 @@ _lib.fa_layer_norm_backward.argtypes = [_vp, _ll, _vp, _ll, _vp, _i, _ll, _ll, _
 _lib.fa_gelu_forward.argtypes = [_vp, _ll, _i, _ll, _ll, _vp, _i, _i, _vp, _ll, _vp, _vp, _vp]
 _lib.fa_gelu_backward_workspace_bytes.argtypes = [_ll, _ll, ctypes.POINTER(_sz)]
 _lib.fa_gelu_backward.argtypes = [_vp, _ll, _vp, _ll, _vp, _i, _vp, _i, _ll, _ll, _i, _vp, _ll, _vp, _i, _vp, _sz, _vp]
-_lib.fa_linear_weight_grad_workspace_bytes.argtypes = [_ll, _ll, _ll, _i, ctypes.POINTER(_sz)]
+_lib.fa_linear_weight_grad_workspace_bytes.argtypes = [_ll, _ll, _ll, _i, _i, ctypes.POINTER(_sz)]
 _lib.fa_linear_weight_grad.argtypes = [_vp, _ll, _i, _ll, _ll, _vp, _ll, _vp, _vp, _i, _vp, _sz, _vp]
 for _name in ("fa_checkpoint8_bytes", "fa_checkpoint8_store", "fa_checkpoint8_load", "fa_layer_norm_forward",
               "fa_layer_norm_backward_workspace_bytes", "fa_layer_norm_backward", "fa_gelu_forward",
@@ -370,8 +370,9 @@ def fa_gelu_backward(dy, x=None, bias=None, ck=None, approximate="tanh", dx=None
     return dx, dbias
 
 
-def fa_linear_weight_grad_workspace_bytes(rows: int, outs: int, ins: int, dtype) -> int:
-    return _bytes_of("fa_linear_weight_grad_workspace_bytes", rows, outs, ins, _CODES[dtype])
+def fa_linear_weight_grad_workspace_bytes(rows: int, outs: int, ins: int, dtype, aligned: bool = False) -> int:
+    """aligned: address and row stride of dy are multiples of 16 bytes."""
+    return _bytes_of("fa_linear_weight_grad_workspace_bytes", rows, outs, ins, _CODES[dtype], 1 if aligned else 0)
 
 
 def fa_linear_weight_grad(dy, ck, ins, dweight=None, dbias=None, ws=None, stream=None):
@@ -384,7 +385,9 @@ def fa_linear_weight_grad(dy, ck, ins, dweight=None, dbias=None, ws=None, stream
         given = dbias
         dbias, dbp = _grad(dbias, (outs,), outs, "dbias", dev, dweight)
         dweight, dwp = _grad(dweight, (outs, ins), outs * ins, "dweight", dev, given)
-        ws, wsp, wsb = _workspace(ws, _bytes_of("fa_linear_weight_grad_workspace_bytes", rows, outs, ins, code), dev)
+        aligned = 0 if dyp % 16 or lddy * dy.element_size() % 16 or lddy < outs else 1
+        nbytes = _bytes_of("fa_linear_weight_grad_workspace_bytes", rows, outs, ins, code, aligned)
+        ws, wsp, wsb = _workspace(ws, nbytes, dev)
         _check(_lib.fa_linear_weight_grad(dyp, lddy, code, rows, outs, cp, ins, dwp, dbp,
                                           _grad_code(dweight, dbias, "dweight and dbias"), wsp, wsb,
                                           _raw_stream(dev.index)), "fa_linear_weight_grad")

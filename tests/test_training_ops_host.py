@@ -31,7 +31,10 @@ def test_size_limits(fa):
     for rows, cols, code in ((-1, 8, ARG), (1, 0, ARG), (1, (1 << 23) + 1, ARG), ((1 << 40) + 1, 8, ARG), (1 << 40, 1 << 23, OK)):
         assert fa._lib.fa_checkpoint8_bytes(rows, cols, ctypes.byref(size)) == code
     assert fa._lib.fa_checkpoint8_bytes(1, 8, None) == ARG
-    assert fa._lib.fa_linear_weight_grad_workspace_bytes(1, 8, 8, 5, ctypes.byref(size)) == ARG
+    assert fa._lib.fa_linear_weight_grad_workspace_bytes(1, 8, 8, 5, 1, ctypes.byref(size)) == ARG
+    # a bf16 dY on 16-byte boundaries needs no room of its own
+    assert fa.fa_linear_weight_grad_workspace_bytes(4096, 4096, 1024, torch.bfloat16, True) < 4096 * 4096 * 2 <= \
+        fa.fa_linear_weight_grad_workspace_bytes(4096, 4096, 1024, torch.bfloat16) < fa.fa_linear_weight_grad_workspace_bytes(4096, 4096, 1024, torch.float32, True)
     for rows in (0, 1, 100_000):
         assert 0 < fa.fa_layer_norm_backward_workspace_bytes(rows, 768) < 64 << 20
         assert 0 < fa.fa_gelu_backward_workspace_bytes(rows, 768) < 64 << 20
