@@ -42,6 +42,7 @@ constexpr int kConvGroups = 3;                       // a group of four warps co
 //     stage's previous phase up;
 //   * `empty` of step n: the group has done step n - kConvGroups, for which products n - kConvGroups - kStages
 //     had ended; with kConvGroups <= kStages that is at most one phase before the one waited for.
+constexpr int kRun = 24;                             // stages of a run of an fp32 sum
 constexpr int kScaleWarp = 6 + 4 * kConvGroups;
 constexpr int kColumnWarp = kScaleWarp + 1;
 // warp 0 dY, 1 MMA, 2-5 read-out, 6.. converters, codes, and (SIDE) four for column sums
@@ -75,8 +76,9 @@ struct Params {
   int planes;                    // terms of dY; every term is a step of its own, with the codes converted anew
   int tiles_i, tiles;            // tiles along the inputs, in all
   int splits;
-  int ksteps;                    // steps in all: stages of tokens x terms
-  int run;                       // steps summed in the accumulator before they are added to the result in fp32
+  int ksteps;                    // stages of tokens in all
+  int run;                       // stages summed in an accumulator, with every term, before they are added in fp32
+  int joint;                     // a unit is at most two runs, and no block has two units: both are read out at once
   void* dw;                      // splits == 1
   int gbf16;
   float* partials;               // splits > 1: [splits][split_stride]
@@ -225,6 +227,25 @@ __device__ __forceinline__ __nv_bfloat162 scale_bf16(uint32_t byte) {
   return *reinterpret_cast<__nv_bfloat162*>(&s);
 }
 
+// The steps of a unit in their order: run by run, and within one the smallest terms first, so that the accumulator is
+// as small as they are while they are added (what it loses by each addition goes by its own size).
+struct Steps {
+  int k, pl;             // stage of tokens, term
+  int r0, r1, run, k1, planes;
+  __device__ __forceinline__ Steps(const Params& p, const Unit& w)
+      : k(w.k0), pl(p.planes - 1), r0(w.k0), r1(min(w.k0 + p.run, w.k1)), run(p.run), k1(w.k1), planes(p.planes) {}
+  __device__ __forceinline__ bool more() const { return r0 < k1; }
+  __device__ __forceinline__ void advance() {
+    if (++k < r1) return;
+    if (--pl < 0) {
+      pl = planes - 1;
+      r0 = r1;
+      r1 = min(r0 + run, k1);
+    }
+    k = r0;
+  }
+};
+
 // Column sums of dY while the products run: the tiles that read the same columns share the steps out among themselves,
 // so that every value of dY is read once more, when it is in L2.  (A pass of its own over dY took 46 us next to 234
 // for 4096 x 1024 outputs and inputs of 32768 tokens; this takes 19.)  Four warps: each takes every fourth pair of
@@ -238,8 +259,8 @@ struct ColumnSums {
   static constexpr int kHalf = kTokens / 16;         // rows of a thread per half step
   // The unit's steps that are this tile's; half a step's loads are always under way.
   __device__ __forceinline__ static void run(const Params& p, const Unit& w, int tile_i, int rank, int warp, int lane) {
-    const int first = w.k0 + tile_i;
-    const int halves = first < w.k1 ? 2 * ((w.k1 - first + p.tiles_i - 1) / p.tiles_i) : 0;
+    const int steps = (w.k1 - w.k0) * p.planes;
+    const int halves = tile_i < steps ? 2 * ((steps - tile_i + p.tiles_i - 1) / p.tiles_i) : 0;
     float* out = p.columns + ((size_t)(w.split * p.tiles_i + tile_i) * 4 + warp) * p.width;
     for (int c = 0; c < kCols; c += 128) {
       const int col = w.o0 + (c >> 7) * (128 * PAIR) + rank * 128 + (lane & 15) * 8;
@@ -248,8 +269,8 @@ struct ColumnSums {
       for (int i = 0; i < 4; ++i) acc[i] = two(0.f);
       Raw8<bf16> raw[2][kHalf];
       auto load = [&](int h, Raw8<bf16> (&r)[kHalf]) {
-        const int j = first + (h >> 1) * p.tiles_i, k = j / p.planes;
-        const bf16* src = p.dy + (long long)(j - k * p.planes) * p.plane;
+        const int j = tile_i + (h >> 1) * p.tiles_i, k = w.k0 + j / p.planes;
+        const bf16* src = p.dy + (long long)(j % p.planes) * p.plane;
         const long long row0 = (long long)k * kTokens + (h & 1) * (kTokens / 2) + 2 * warp + (lane >> 4);
 #pragma unroll
         for (int q = 0; q < kHalf; ++q) {
@@ -341,8 +362,8 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
       bool ok = true;
       for (int u = first_unit; u < units && ok; u += unit_step) {
         const Unit w = unit_of<N, PAIR>(prm, u, rank);
-        int k = w.k0 / prm.planes, pl = w.k0 - k * prm.planes;
-        for (int j = w.k0; j < w.k1; ++j, ++n) {
+        Steps at(prm, w);
+        for (; at.more(); at.advance(), ++n) {
           const int s = n % C::kStages;
           ok = mbar_wait(&bars->empty[s], ((n / C::kStages) & 1) ^ 1);
           if (!ok) break;
@@ -350,9 +371,8 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
           unsigned char* b = stages + (size_t)s * C::kStage + kBytesA;
 #pragma unroll
           for (int q = 0; q < N / PAIR / 64; ++q)
-            tma_load_3d<PAIR>(b + q * kBoxBytes, &map_dy, w.o0 + (q >> 1) * (128 * PAIR) + rank * 128 + (q & 1) * 64, k * kTokens, pl,
-                              &bars->full[s]);
-          if (++pl == prm.planes) { pl = 0; ++k; }
+            tma_load_3d<PAIR>(b + q * kBoxBytes, &map_dy, w.o0 + (q >> 1) * (128 * PAIR) + rank * 128 + (q & 1) * 64, at.k * kTokens,
+                              at.pl, &bars->full[s]);
         }
       }
       // copies still in flight must land before the block may exit
@@ -369,10 +389,10 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
       for (int u = first_unit; u < units && ok; u += unit_step) {
         const Unit w = unit_of<N, PAIR>(prm, u, rank);
         for (int j0 = w.k0; j0 < w.k1 && ok; j0 += prm.run, ++nu) {
-          const int j1 = min(j0 + prm.run, w.k1);
+          const int steps = (min(j0 + prm.run, w.k1) - j0) * prm.planes;
           const uint32_t acc = nu % C::kAccs, d = tmem_base + acc * N;
           ok = mbar_wait(&bars->acc_empty[acc], ((nu / C::kAccs) & 1) ^ 1);
-          for (int j = j0; j < j1 && ok; ++j, ++n) {
+          for (int j = 0; j < steps && ok; ++j, ++n) {
             const int s = n % C::kStages;
             ok = mbar_wait(&bars->full[s], (n / C::kStages) & 1);
             if (!ok) break;
@@ -383,7 +403,7 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
 #pragma unroll
               for (int h = 0; h < N / C::kMma; ++h)
                 umma<PAIR>(d + h * C::kMma, mn_desc(a + q * 2048), mn_desc(b + h * (C::kMma / PAIR / 64) * kBoxBytes + q * 2048),
-                           C::kIdesc, (j == j0 && q == 0) ? 0u : 1u);
+                           C::kIdesc, (j == 0 && q == 0) ? 0u : 1u);
             umma_commit<PAIR>(&bars->empty[s]);
           }
           if (ok) umma_commit<PAIR>(&bars->acc_full[acc]);
@@ -398,10 +418,10 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
   } else if (warp < 6) {
     // ---------------- read-out: warp w reads the 32 accumulator rows of its quarter.  The tensor cores cut the sums
     // off rather than rounding them, an error that grows with the number of additions (1.8e-5 of the result after
-    // 32768 tokens), so a sum wanted in fp32 is formed in runs (4.5e-7): the first is stored, the others are added to
-    // it in L2.  Only this thread ever touches the element, one run after the other, so the order is fixed; an
-    // atomic addition is used because nothing has to wait for it (a load, add and store took 100 us of 590 for
-    // 16384 x 4096 x 4096).
+    // 32768 tokens), so a sum wanted in fp32 is formed in runs (7e-7).  Two runs and no more: one in each accumulator,
+    // added here.  Otherwise the first is stored, the others are added to it in L2: only this thread ever touches the
+    // element, one run after the other, so the order is fixed; an atomic addition is used because nothing has to wait
+    // for it (a load, add and store took 100 us of 590 for 16384 x 4096 x 4096).
     const int quarter = warp & 3;
     uint32_t nu = 0;
     bool ok = true;
@@ -412,15 +432,25 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
       const bool to_bf16 = prm.splits == 1 && prm.gbf16;
       if (!SIDE && prm.columns)
         ColumnSums<N, PAIR>::run(prm, w, (u - w.split * prm.tiles) % prm.tiles_i, rank, warp & 3, lane);
-      for (int j0 = w.k0; j0 < w.k1; j0 += prm.run, ++nu) {
+      for (int j0 = w.k0; j0 < w.k1;) {
+        const bool two_runs = prm.joint && j0 + prm.run < w.k1;
         const uint32_t acc = nu % C::kAccs;
         ok = __all_sync(0xffffffffu, ok && mbar_wait(&bars->acc_full[acc], (nu / C::kAccs) & 1));
+        if (C::kAccs == 2 && two_runs) ok = __all_sync(0xffffffffu, ok && mbar_wait(&bars->acc_full[acc ^ 1], ((nu + 1) >> 1) & 1));
         tc_fence_after();
         for (int c = 0; c < N; c += 32) {
+          const uint32_t at_lane = tmem_base + (static_cast<uint32_t>(32 * quarter) << 16) + c;
           uint32_t v[32];
           if (ok) {
-            tmem_ld32(tmem_base + (static_cast<uint32_t>(32 * quarter) << 16) + acc * N + c, v);
+            tmem_ld32(at_lane + acc * N, v);
             asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+            if (C::kAccs == 2 && two_runs) {
+              uint32_t u[32];
+              tmem_ld32(at_lane + (acc ^ 1) * N, u);
+              asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(u[j]));
+            }
           } else {                                     // a wait ran out: the result shows it
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = 0x7FC00000u;
@@ -445,7 +475,12 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) arrive_first<PAIR>(&bars->acc_empty[acc]);
+        if (lane == 0) {
+          arrive_first<PAIR>(&bars->acc_empty[acc]);
+          if (C::kAccs == 2 && two_runs) arrive_first<PAIR>(&bars->acc_empty[acc ^ 1]);
+        }
+        nu += two_runs ? 2 : 1;
+        j0 += two_runs ? 2 * prm.run : prm.run;
       }
     }
   } else if (warp < kScaleWarp) {
@@ -457,7 +492,7 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
     int total = 0;
     for (int u = first_unit; u < units; u += unit_step) {
       const Unit w = unit_of<N, PAIR>(prm, u, rank);
-      total += w.k1 - w.k0;
+      total += (w.k1 - w.k0) * prm.planes;
     }
     for (int n = (warp - 6) >> 2; n < total; n += kConvGroups) {
       const int s = n % C::kStages, r = n % C::kStagesRaw;
@@ -506,28 +541,26 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
       const Unit w = unit_of<N, PAIR>(prm, u, rank);
       // (the second block of a pair may have no inputs at all: its results are not stored)
       const uint8_t* column = prm.scales + ((w.i0 >> 5) < prm.scale_pitch ? w.i0 >> 5 : 0);
-      int k = w.k0 / prm.planes, pl = w.k0 - k * prm.planes;
-      for (int j = w.k0; j < w.k1; ++j, ++n) {
+      for (Steps at(prm, w); at.more(); at.advance(), ++n) {
         const int r = n % C::kStagesRaw;
         ok = __all_sync(0xffffffffu, mbar_wait(&bars->raw_empty[r], ((n / C::kStagesRaw) & 1) ^ 1));
         if (!ok) break;
         if (leader) {
           mbar_arrive_expect_tx(&bars->raw_full[r], kCodeBytes);
-          tma_load_2d(raws + (size_t)r * kRawBytes, &map_codes, w.i0, k * kTokens, &bars->raw_full[r]);
+          tma_load_2d(raws + (size_t)r * kRawBytes, &map_codes, w.i0, at.k * kTokens, &bars->raw_full[r]);
         }
         __syncwarp();
         const uint32_t dst = smem_u32(raws + (size_t)r * kRawBytes + kCodeBytes);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int t = lane + h * 32;
-          const long long row = (long long)k * kTokens + t;
+          const long long row = (long long)at.k * kTokens + t;
           const bool inside = row < prm.rows;
           asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst + t * 4),
                        "l"(column + (size_t)(inside ? row : 0) * prm.scale_pitch), "r"(inside ? 4 : 0)
                        : "memory");
         }
         asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&bars->raw_full[r])) : "memory");
-        if (++pl == prm.planes) { pl = 0; ++k; }
       }
     }
     // nothing may be in flight when the block exits: the codes of every step have to have landed
@@ -640,7 +673,7 @@ Plan plan_of(long long rows, long long outs, long long ins, int dtype, int gdtyp
   p.pack = pack;
   p.pitch = static_cast<int>((outs + 7) / 8 * 8);
   p.pack_bytes = pack ? ((size_t)p.planes * rows * p.pitch * 2 + 255) / 256 * 256 : 0;
-  p.ksteps = static_cast<int>((rows + kTokens - 1) / kTokens) * p.planes;
+  p.ksteps = static_cast<int>((rows + kTokens - 1) / kTokens);
   auto cut = [&](int n, int pair, double step) {
     p.n = n;
     p.pair = pair;
@@ -650,13 +683,15 @@ Plan plan_of(long long rows, long long outs, long long ins, int dtype, int gdtyp
     p.tiles = static_cast<int>(tiles);
     // splits that fill the blocks once; each keeps at least 4 stages
     long long s = tiles >= blocks ? 1 : blocks / tiles;
-    if (s > (p.ksteps + 3) / 4) s = (p.ksteps + 3) / 4;
+    const long long least = (p.ksteps * p.planes + 3) / 4;
+    if (s > least) s = least;
+    if (s > p.ksteps) s = p.ksteps;
     if (s > 32) s = 32;
     p.splits = static_cast<int>(s < 1 ? 1 : s);
     // time of the busiest block in steps with 256 outputs (0.47 us), and what writing, reading and adding the splits
     // costs in these (2 TB/s: little of it is hidden)
     const long long turns = (tiles * p.splits + blocks - 1) / blocks;
-    return (double)turns * ((p.ksteps + p.splits - 1) / p.splits) * step +
+    return (double)turns * ((p.ksteps + p.splits - 1) / p.splits) * p.planes * step +
            (p.splits > 1 ? (double)p.splits * outs * ins * 8.0 / 2e6 / 0.47 : 0.0);
   };
   // Tiles of 128 x 128 by single blocks where there is little to do: more blocks share the read-out, and no pair has to
@@ -764,7 +799,12 @@ cudaError_t launch_linear_weight_grad(Mat dy, int dtype, long long rows, long lo
   prm.planes = p.planes;
   prm.tiles_i = p.tiles_i; prm.tiles = p.tiles; prm.splits = p.splits; prm.ksteps = p.ksteps;
   prm.dw = dweight; prm.gbf16 = gdtype == FA_BF16;
-  prm.run = gdtype == FA_BF16 ? p.ksteps : 32;      // (a bf16 result is rounded to 2^-9 anyway)
+  const int steps = (p.ksteps + p.splits - 1) / p.splits;
+  prm.run = steps;                                  // (a bf16 result is rounded to 2^-9 anyway)
+  if (gdtype != FA_BF16) {
+    prm.joint = steps <= 2 * wgrad::kRun && p.tiles * (long long)p.splits <= sm_count() / p.pair;
+    prm.run = prm.joint ? (steps + 1) / 2 : wgrad::kRun;
+  }
   char* room = static_cast<char*>(scratch) + p.pack_bytes;
   prm.partials = reinterpret_cast<float*>(room);
   prm.split_stride = p.split_stride;
@@ -773,7 +813,7 @@ cudaError_t launch_linear_weight_grad(Mat dy, int dtype, long long rows, long lo
   prm.plane = ld * rows;
   prm.columns = dbias ? reinterpret_cast<float*>(room + p.partial_bytes) : nullptr;
   prm.width = p.pitch;
-  const bool side = dbias && (p.ksteps + p.splits - 1) / p.splits > prm.run;
+  const bool side = dbias && steps > prm.run && !prm.joint;
   auto go = [&](auto with_side) {
     constexpr bool SIDE = decltype(with_side)::value;
     return p.n == 512   ? launch_product<512, 2, SIDE>(map, map_codes, prm, st)

@@ -400,7 +400,7 @@ def test_linear_weight_grad_of_many_products(dtype, gdtype, rows, outs, ins):
     exact, mags = dy.double().T @ x, dy.double().abs().T @ x.abs()
     units = 2 * (rows / 16 + 34) + 16                            # as above
     ref.assert_close(dw, exact, mags, units, "dweight")
-    if gdtype == "f32":      # summed in runs of 32 steps: 512 additions at two units, then at most rows / 2048 + 34 more
+    if gdtype == "f32":      # summed in runs of at most 512 additions at two units, then at most rows / 512 + 34 more
         ref.assert_close(dw, exact, mags, 2 * (512 + rows / 512 + 34), "dweight in runs")
     ref.assert_close(db, dy.double().sum(0), dy.double().abs().sum(0), rows / 8 + 128, "dbias")
     assert torch.isnan(row[:1]).all() and torch.isnan(row[1 + outs * (ins + 1):]).all()
