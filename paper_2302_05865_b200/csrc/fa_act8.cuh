@@ -191,9 +191,9 @@ struct Source {
 
 // Elements first .. first + 7 of a row of `cols`, zeros past its end: fetched now, put together when they are needed, so
 // that a fetch waits for nothing.  VEC: rows start on 16-byte boundaries and cols is a multiple of 8, so a chunk is one
-// aligned load (fp32: two), or lies outside.  Otherwise it is cut out of the aligned 16-byte blocks it lies in, where
-// these are inside the matrix (from its first element to its last, the gaps between rows included); the one or two
-// chunks of a whole matrix where they are not are read element by element.
+// aligned load (fp32: two), or lies outside.  Otherwise it is cut out of the aligned 16-byte blocks its elements lie in,
+// where these are inside the matrix (from its first element to its last; a block may reach over a row's end); the one
+// or two chunks of a whole matrix where they are not are read element by element.
 template <typename T, bool VEC>
 struct Chunk {
   Raw8<T> r;
@@ -220,12 +220,14 @@ struct Chunk<T, false> {
   __device__ __forceinline__ void fetch(const Source<T>& m, const T* row, int first, int cols) {
     p = row + first;
     valid = cols - first;
-    const T* a = p - (static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) & 15u) / sizeof(T);
-    whole = valid > 0 && a >= m.p && a + 8 + kPer <= m.end;
-    const uint4* b = whole ? reinterpret_cast<const uint4*>(a) : kZeroBlocks;
+    const int before = static_cast<int>((static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) & 15u) / sizeof(T));
+    const T* a = p - before;
+    const int used = before + min(valid, 8);             // elements from the first block's start to the chunk's end
+    whole = valid > 0 && a >= m.p && a + (used + kPer - 1) / kPer * kPer <= m.end;
 #pragma unroll
     for (int i = 0; i < kOut / 4 + 1; ++i) {
-      const uint4 t = b[i];
+      // (a block without an element of the chunk is not read: behind the row there may be nothing)
+      const uint4 t = *(whole && i * kPer < used ? reinterpret_cast<const uint4*>(a) + i : kZeroBlocks + i);
       w[4 * i] = t.x; w[4 * i + 1] = t.y; w[4 * i + 2] = t.z; w[4 * i + 3] = t.w;
     }
   }
