@@ -16,6 +16,9 @@
 // multiplied with each; the same pass lays out a bf16 dY whose rows TMA cannot address.
 // Few tiles and many tokens: the tokens are split over the blocks, partial products go to scratch in
 // fp32 and a second kernel adds them in a fixed order.
+// Shared memory bounds it (see Cfg), and the power limit in a long run.  Measured with the bias gradient, bf16:
+// 4096 x 4096 from 16384 tokens 377 us, 1457 TFLOP/s (439 us in a run of half a second), 4096 x 1024 from 32768 tokens
+// 241 us (278), 768 x 768 from 16384 into fp32 33 us (590 TFLOP/s: 32 steps a pair of blocks, and joining 8 splits).
 #include <cuda.h>
 
 #include <type_traits>
@@ -35,6 +38,7 @@ constexpr int kBoxBytes = 64 * kTokens * 2;          // 64 columns x 64 tokens o
 constexpr int kBytesA = 2 * kBoxBytes;
 constexpr int kCodeBytes = kIns * kTokens;           // codes of a stage as they are stored
 constexpr int kRawBytes = kCodeBytes + 4 * kTokens;  // and the scales of the tile's four groups, a word per token
+constexpr int kRun = 24;                             // most stages of a run of an fp32 sum
 constexpr int kConvGroups = 3;                       // a group of four warps converts every third step
 // A wait tells two neighbouring phases of a barrier apart and no more, so a role must not be able to arrive at a
 // barrier two phases early.  For the converter groups, which skip steps:
@@ -42,7 +46,6 @@ constexpr int kConvGroups = 3;                       // a group of four warps co
 //     stage's previous phase up;
 //   * `empty` of step n: the group has done step n - kConvGroups, for which products n - kConvGroups - kStages
 //     had ended; with kConvGroups <= kStages that is at most one phase before the one waited for.
-constexpr int kRun = 24;                             // stages of a run of an fp32 sum
 constexpr int kScaleWarp = 6 + 4 * kConvGroups;
 constexpr int kColumnWarp = kScaleWarp + 1;
 // warp 0 dY, 1 MMA, 2-5 read-out, 6.. converters, codes, and (SIDE) four for column sums
