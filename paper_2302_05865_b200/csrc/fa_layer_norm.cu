@@ -12,8 +12,8 @@
 //   forward with residual, sum and two checkpoints 137 us (5.0 TB/s, 0.75 of a copy; 44 instructions a value, 62 % of
 //   the issue slots), backward from a checkpoint with residual gradient 108 + 5 us (4.3 TB/s, 0.64; 33 a value),
 // and of 768: 33 and 35 us (0.59, 0.39).  More chunks a thread spread those instructions over more values, fewer leave
-// registers for more warps: four (three) chunks are best in the forward pass (768 columns: 33 us, with one 41), one or
-// two, with two sums a column to keep, in the backward pass.
+// registers for more warps: four (three) chunks are best in the forward pass (768 columns: 33 us, with one 41), one
+// (up to 1024 columns) or two, with two sums a column to keep, in the backward pass.
 #include "../../include/fa.h"
 #include "fa_columns.cuh"
 #include "fa_train.h"
@@ -612,12 +612,12 @@ ln::Shape ln_shape(long long rows, long long cols) {
 }
 
 // Threads per row and chunks (8 values) per thread; false: the row does not fit.  `few` and `many`: chunks per
-// thread of rows of up to 256 chunks, and of longer ones.
-bool ln_team(ln::Shape* s, bool vec, int few, int many, int max_k, int* K) {
+// thread of rows of up to `limit` chunks, and of longer ones.
+bool ln_team(ln::Shape* s, bool vec, int limit, int few, int many, int max_k, int* K) {
   const int chunks = s->width / 8;
   if (chunks > ln::kBlock * max_k) return false;
   // up to one row per SM there is only the one row's latency to shorten: as many threads as it has chunks
-  *K = s->rows <= sm_count() ? 1 : chunks <= 256 ? few : many;
+  *K = s->rows <= sm_count() ? 1 : chunks <= limit ? few : many;
   while (*K * ln::kBlock < chunks) *K *= 2;
   while (*K > 1 && chunks <= 32 * (*K / 2)) *K /= 2;
   auto places = [&](int k) { return ((chunks + k - 1) / k + 31) / 32 * 32 * k; };
@@ -646,7 +646,7 @@ cudaError_t ln_forward_t(const ln::Forward<T>& a, long long rows, long long cols
   ln::Shape s = ln_shape(rows, cols);
   int K = 1;
   const int few = sizeof(T) == 4 ? 1 : VEC ? 4 : 2, many = sizeof(T) == 2 && VEC ? 4 : 2;
-  if (!ln_team(&s, VEC, few, many, ln::kMaxKForward, &K)) {
+  if (!ln_team(&s, VEC, 256, few, many, ln::kMaxKForward, &K)) {
     const unsigned grid = static_cast<unsigned>(rows < (1 << 30) ? rows : 1 << 30);
     ln::forward_long_kernel<T, VEC><<<grid, ln::kBlock, 0, st>>>(a, s);
     return cudaGetLastError();
@@ -693,7 +693,9 @@ struct LnBackwardGrid {
 LnBackwardGrid ln_backward_grid(bool vec, int dtype, long long rows, long long cols) {
   LnBackwardGrid g{};
   g.s = ln_shape(rows, cols);
-  g.is_long = !ln_team(&g.s, vec, 1, 2, ln::kMaxKBackward, &g.K);
+  // bf16: 16384 x 1024 from a checkpoint 42.0 us with one chunk a thread, 41.8 with two; x 1536 58.4 and 54.3; x 2048
+  // 72.6 and 64.5.  An fp32 chunk takes twice the registers on its way: one a thread up to 256 of them.
+  g.is_long = !ln_team(&g.s, vec, dtype == FA_BF16 && vec ? 128 : 256, 1, 2, ln::kMaxKBackward, &g.K);
   long long want;
   if (g.is_long) {
     const long long tiles = (g.s.width + 255) / 256;
