@@ -38,7 +38,13 @@ constexpr int kBoxBytes = 64 * kTokens * 2;          // 64 columns x 64 tokens o
 constexpr int kBytesA = 2 * kBoxBytes;
 constexpr int kCodeBytes = kIns * kTokens;           // codes of a stage as they are stored
 constexpr int kRawBytes = kCodeBytes + 4 * kTokens;  // and the scales of the tile's four groups, a word per token
-constexpr int kRun = 24;                             // most stages of a run of an fp32 sum
+// Most stages of a run.  The tensor cores cut their sums off rather than rounding them, an error that grows with the
+// number of additions: 3.1e-7 of a result (inputs of random sign) after 24 stages and in proportion beyond.  So sums are
+// read out in runs, whatever the type of the result, and the runs added in fp32.  A bf16 result takes longer ones, off by
+// 8e-7, about as a plain fp32 product is: 4096 x 1024 from 32768 tokens 368 us in runs of 24, 270 in runs of 64, 255 in
+// one; 4096 x 4096 from 16384 700, 508 and 390.  In one run the error would have no bound: after 131072 tokens 1.7 % of
+// the results are rounded to another value, in runs of 64 0.07 %.
+constexpr int kRunF32 = 24, kRunBf16 = 64;
 constexpr int kConvGroups = 3;                       // a group of four warps converts every third step
 // A wait tells two neighbouring phases of a barrier apart and no more, so a role must not be able to arrive at a
 // barrier two phases early.  For the converter groups, which skip steps:
@@ -82,9 +88,9 @@ struct Params {
   int ksteps;                    // stages of tokens in all
   int run;                       // stages summed in an accumulator, with every term, before they are added in fp32
   int joint;                     // a unit is at most two runs, and no block has two units: both are read out at once
-  void* dw;                      // splits == 1
+  void* dw;
   int gbf16;
-  float* partials;               // splits > 1: [splits][split_stride]
+  float* partials;               // fp32 sums [splits][split_stride] for the finishing kernel; null: formed in dw
   size_t split_stride;
   const bf16* dy;                // what map_dy reads: rows `ld`, terms `plane` elements apart
   long long ld, plane;
@@ -419,20 +425,19 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
     }
     __syncwarp();
   } else if (warp < 6) {
-    // ---------------- read-out: warp w reads the 32 accumulator rows of its quarter.  The tensor cores cut the sums
-    // off rather than rounding them, an error that grows with the number of additions (1.8e-5 of the result after
-    // 32768 tokens), so a sum wanted in fp32 is formed in runs (7e-7).  Two runs and no more: one in each accumulator,
-    // added here.  Otherwise the first is stored, the others are added to it in L2: only this thread ever touches the
-    // element, one run after the other, so the order is fixed; an atomic addition is used because nothing has to wait
-    // for it (a load, add and store took 100 us of 590 for 16384 x 4096 x 4096).
+    // ---------------- read-out: warp w reads the 32 accumulator rows of its quarter, run by run (see kRunF32).  Two runs
+    // and no more: one in each accumulator, added here.  Otherwise the first is stored in fp32, the others are added to
+    // it in L2: only this thread ever touches the element, one run after the other, so the order is fixed; an atomic
+    // addition is used because nothing has to wait for it (a load, add and store took 100 us of 590 for
+    // 16384 x 4096 x 4096).
     const int quarter = warp & 3;
     uint32_t nu = 0;
     bool ok = true;
     for (int u = first_unit; u < units; u += unit_step) {
       const Unit w = unit_of<N, PAIR>(prm, u, rank);
       const int i = w.i0 + quarter * 32 + lane;
-      float* sums = prm.splits > 1 ? prm.partials + (size_t)w.split * prm.split_stride : static_cast<float*>(prm.dw);
-      const bool to_bf16 = prm.splits == 1 && prm.gbf16;
+      float* sums = prm.partials ? prm.partials + (size_t)w.split * prm.split_stride : static_cast<float*>(prm.dw);
+      const bool to_bf16 = prm.gbf16 && !prm.partials;
       if (!SIDE && prm.columns)
         ColumnSums<N, PAIR>::run(prm, w, (u - w.split * prm.tiles) % prm.tiles_i, rank, warp & 3, lane);
       for (int j0 = w.k0; j0 < w.k1;) {
@@ -664,12 +669,15 @@ constexpr double kWideStep = 1.55;       // time of a step with 512 outputs, in 
 // a write and a read of the whole result.
 struct Plan {
   int n, pair, tiles_i, tiles_o, tiles, splits, ksteps, planes;
+  int run;
+  bool joint;
+  bool several;        // units are read out more than once: of a bf16 result through fp32 sums and the finishing kernel
   bool pack;
   int pitch;
   size_t pack_bytes, split_stride, partial_bytes, column_bytes;
 };
 
-// `gdtype` of the result: one in fp32 is read out in runs, which a tile of 512 outputs would have to wait for.
+// `gdtype` of the result: one in fp32 is read out in short runs, for which a tile of 512 outputs would have to wait.
 Plan plan_of(long long rows, long long outs, long long ins, int dtype, int gdtype, bool pack) {
   Plan p{};
   p.planes = dtype == FA_F32 ? 3 : 1;
@@ -704,8 +712,12 @@ Plan plan_of(long long rows, long long outs, long long ins, int dtype, int gdtyp
   const int n = little || outs <= 128 ? 128 : 256, pair = !little && ins > kIns && outs > 128 ? 2 : 1;
   const double cost = cut(n, pair, 1.0);
   if (pair == 2 && outs > 256 && gdtype == FA_BF16 && cut(512, 2, kWideStep) >= cost) cut(n, pair, 1.0);
+  const int steps = (p.ksteps + p.splits - 1) / p.splits, most = gdtype == FA_BF16 ? kRunBf16 : kRunF32;
+  p.joint = p.n <= 256 && steps <= 2 * most && p.tiles * (long long)p.splits <= sm_count() / p.pair;
+  p.run = p.joint ? (steps + 1) / 2 : most;
+  p.several = !p.joint && steps > most;
   p.split_stride = ((size_t)outs * ins + 63) / 64 * 64;
-  p.partial_bytes = p.splits > 1 ? p.splits * p.split_stride * sizeof(float) : 0;
+  p.partial_bytes = p.splits > 1 || (p.several && gdtype == FA_BF16) ? p.splits * p.split_stride * sizeof(float) : 0;
   p.column_bytes = (size_t)p.splits * p.tiles_i * 4 * p.pitch * sizeof(float);
   return p;
 }
@@ -802,21 +814,16 @@ cudaError_t launch_linear_weight_grad(Mat dy, int dtype, long long rows, long lo
   prm.planes = p.planes;
   prm.tiles_i = p.tiles_i; prm.tiles = p.tiles; prm.splits = p.splits; prm.ksteps = p.ksteps;
   prm.dw = dweight; prm.gbf16 = gdtype == FA_BF16;
-  const int steps = (p.ksteps + p.splits - 1) / p.splits;
-  prm.run = steps;                                  // (a bf16 result is rounded to 2^-9 anyway)
-  if (gdtype != FA_BF16) {
-    prm.joint = steps <= 2 * wgrad::kRun && p.tiles * (long long)p.splits <= sm_count() / p.pair;
-    prm.run = prm.joint ? (steps + 1) / 2 : wgrad::kRun;
-  }
+  prm.run = p.run; prm.joint = p.joint;
   char* room = static_cast<char*>(scratch) + p.pack_bytes;
-  prm.partials = reinterpret_cast<float*>(room);
+  prm.partials = p.partial_bytes ? reinterpret_cast<float*>(room) : nullptr;
   prm.split_stride = p.split_stride;
   prm.dy = static_cast<const bf16*>(base);
   prm.ld = ld;
   prm.plane = ld * rows;
   prm.columns = dbias ? reinterpret_cast<float*>(room + p.partial_bytes) : nullptr;
   prm.width = p.pitch;
-  const bool side = dbias && steps > prm.run && !prm.joint;
+  const bool side = dbias && p.several;
   auto go = [&](auto with_side) {
     constexpr bool SIDE = decltype(with_side)::value;
     return p.n == 512   ? launch_product<512, 2, SIDE>(map, map_codes, prm, st)
@@ -825,14 +832,14 @@ cudaError_t launch_linear_weight_grad(Mat dy, int dtype, long long rows, long lo
                         : launch_product<128, 1, SIDE>(map, map_codes, prm, st);
   };
   const cudaError_t e = side ? go(std::true_type{}) : go(std::false_type{});
-  if (e != cudaSuccess || (p.splits == 1 && !dbias)) return e;
+  if (e != cudaSuccess || (!prm.partials && !dbias)) return e;
   wgrad::Finish f{};
   f.partials = prm.partials; f.split_stride = p.split_stride; f.n = n; f.splits = p.splits;
   f.dw = dweight;
   f.columns = prm.columns; f.parts = p.splits * p.tiles_i * 4; f.width = p.pitch; f.outs = (int)outs;
   f.db = dbias;
   f.gbf16 = prm.gbf16;
-  f.product_blocks = p.splits > 1 ? (unsigned)((n + 255) / 256) : 0;
+  f.product_blocks = prm.partials ? (unsigned)((n + 255) / 256) : 0;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(f.product_blocks + (dbias ? (unsigned)((outs + 31) / 32) : 0));
   cfg.blockDim = dim3(256);
