@@ -117,10 +117,11 @@ __device__ __forceinline__ ParamCache cache_param(float* room, const ParamVec& w
   return c;
 }
 
-// Quotient of a sum and the number of columns, to the last bit but for rare ties; exact where it is a float.
+// Quotient of a sum and the number of columns, to the last bit but for rare ties; exact where it is a float.  That of an
+// infinite sum has no remainder.
 __device__ __forceinline__ float mean_of(float sum, const Shape& s) {
   const float q = sum * s.inv;
-  return fmaf(fmaf(-q, s.n, sum), s.inv, q);
+  return fabsf(q) <= 3.402823466e38f ? fmaf(fmaf(-q, s.n, sum), s.inv, q) : q;
 }
 
 // 1 / sqrt(v), rounded to nearest but for rare ties: an error of rstd is shared by its whole row, and rsqrtf's is up to
