@@ -666,15 +666,20 @@ cudaError_t ln_forward_t(const ln::Forward<T>& a, long long rows, long long cols
   const long long want = (rows + teams - 1) / teams, most = sm_count();
   const unsigned grid = static_cast<unsigned>(want < most ? want : most);
   const size_t smem = 2 * (size_t)s.width * sizeof(float);
-  auto go = [&](auto kernel) {
-    if (smem > 32 << 10) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  // The attribute belongs to the kernel: always what its widest row takes, so that calls of several threads agree.
+  auto go = [&](auto kernel, int k) {
+    const size_t most = 2 * (size_t)k * ln::kBlock * 8 * sizeof(float);
+    if (most > 32 << 10) {
+      const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most));
+      if (e != cudaSuccess) return e;
+    }
     kernel<<<grid, threads, smem, st>>>(a, s);
+    return cudaGetLastError();
   };
-  if (K == 1) go(ln::forward_kernel<T, VEC, 1>);
-  else if (K == 2) go(ln::forward_kernel<T, VEC, 2>);
-  else if (K == 3) go(ln::forward_kernel<T, VEC, 3>);
-  else go(ln::forward_kernel<T, VEC, 4>);
-  return cudaGetLastError();
+  return K == 1   ? go(ln::forward_kernel<T, VEC, 1>, 1)
+         : K == 2 ? go(ln::forward_kernel<T, VEC, 2>, 2)
+         : K == 3 ? go(ln::forward_kernel<T, VEC, 3>, 3)
+                  : go(ln::forward_kernel<T, VEC, 4>, 4);
 }
 
 template <typename T>
@@ -731,12 +736,12 @@ cudaError_t ln_backward_t(const ln::Backward<T>& a, const LnBackwardGrid& g, flo
     const dim3 grid(g.grid, (g.s.width + 255) / 256);
     ln::backward_long_kernel<T, VEC, CK><<<grid, 256, 0, st>>>(a, g.s, row_stats);
   } else {
+    // a team's row has at most 8 K values a thread: at most 32 KB with 512 threads of K = 2 and less with others, which
+    // needs no attribute
+    static_assert(ln::kBlock * 8 * ln::kMaxKBackward * sizeof(float) <= 32 << 10 && 768 * 8 * sizeof(float) <= 32 << 10, "");
     const size_t smem = (size_t)g.s.width * sizeof(float) +
                         (a.partials ? (size_t)(g.teams - 1) * g.s.team * 8 * g.K * sizeof(float) : 0);
-    auto go = [&](auto kernel) {
-      if (smem > 32 << 10) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-      kernel<<<g.grid, g.threads, smem, st>>>(a, g.s);
-    };
+    auto go = [&](auto kernel) { kernel<<<g.grid, g.threads, smem, st>>>(a, g.s); };
     if (g.K == 1) go(ln::backward_kernel<T, VEC, 1, CK>);
     else go(ln::backward_kernel<T, VEC, 2, CK>);
   }
