@@ -405,12 +405,6 @@ struct RawAct8 {
       v[2 + i] = mul2(add2(two(spread(b, 2 * i), spread(b, 2 * i + 1)), off), s);
     }
   }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
-    F2 u[4];
-    get(u);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) apart(u[i], &v[2 * i], &v[2 * i + 1]);
-  }
 };
 // ---- division by a number fixed per launch, for 0 <= n < 2^31
 struct FastDiv {
