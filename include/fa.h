@@ -281,7 +281,8 @@ int fa_gelu_backward(const void* dy, long long lddy, const void* x, long long ld
  * of rounding, over at most 1536 (fp32 result) or 4096 (bf16) tokens, and of these rounded to nearest; for inputs of
  * random sign that is 3e-7 and 8e-7 of the result, whatever their number.  A device wait that runs out leaves NaN in
  * the results it concerns.  ws: fa_linear_weight_grad_workspace_bytes(); aligned: non-zero if address and row stride of
- * dy are multiples of 16 bytes (a bf16 dy is then read where it lies; any other is laid out in the workspace first). */
+ * dy are multiples of 16 bytes and the row stride is at least outs (a bf16 dy is then read where it lies; any other, one
+ * row for all included, is laid out in the workspace first). */
 #define FA_MAX_TOKENS 2147483520LL     /* 2^31 - 128 */
 int fa_linear_weight_grad_workspace_bytes(long long rows, long long outs, long long ins, int dtype, int aligned,
                                           size_t* bytes);

@@ -371,7 +371,7 @@ def fa_gelu_backward(dy, x=None, bias=None, ck=None, approximate="tanh", dx=None
 
 
 def fa_linear_weight_grad_workspace_bytes(rows: int, outs: int, ins: int, dtype, aligned: bool = False) -> int:
-    """aligned: address and row stride of dy are multiples of 16 bytes."""
+    """aligned: address and row stride of dy are multiples of 16 bytes, and the row stride is at least outs."""
     return _bytes_of("fa_linear_weight_grad_workspace_bytes", rows, outs, ins, _CODES[dtype], 1 if aligned else 0)
 
 
