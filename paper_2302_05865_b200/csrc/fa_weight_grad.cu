@@ -21,6 +21,7 @@
 // 241 us (278), 768 x 768 from 16384 into fp32 33 us (590 TFLOP/s: 32 steps a pair of blocks, and joining 8 splits).
 #include <cuda.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "../../include/fa.h"
@@ -52,6 +53,7 @@ constexpr int kConvGroups = 3;                       // a group of four warps co
 //     stage's previous phase up;
 //   * `empty` of step n: the group has done step n - kConvGroups, for which products n - kConvGroups - kStages
 //     had ended; with kConvGroups <= kStages that is at most one phase before the one waited for.
+constexpr long long kLandCycles = 1LL << 24;         // ~9 ms: far more than any copy takes
 constexpr int kScaleWarp = 6 + 4 * kConvGroups;
 constexpr int kColumnWarp = kScaleWarp + 1;
 // warp 0 dY, 1 MMA, 2-5 read-out, 6.. converters, codes, and (SIDE) four for column sums
@@ -96,6 +98,7 @@ struct Params {
   long long ld, plane;
   float* columns;                // column sums of dY: [splits * tiles_i * 4][width], or null
   int width;                     // outs rounded up to 8
+  long long wait_cycles;         // limit of a wait (kWaitCycles unless a test shortened it)
 };
 
 template <int N, int PAIR>
@@ -362,8 +365,9 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
   sync_all<PAIR>();
   tc_fence_after();
   const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t*>(&bars->tmem_base);
-  // Every wait is bounded.  A role whose wait ran out leaves its loop, the others' waits then run out as
+  // Every wait is bounded.  A role whose wait ran out arrives nowhere any more, the others' waits then run out as
   // well, and the read-out writes NaN.  (A shared flag looked at after every wait cost 8 % of the run time.)
+  auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity, prm.wait_cycles); };
   if (warp == 0) {
     // ---------------- dY by TMA
     if (elect_one()) {
@@ -374,7 +378,7 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
         Steps at(prm, w);
         for (; at.more(); at.advance(), ++n) {
           const int s = n % C::kStages;
-          ok = mbar_wait(&bars->empty[s], ((n / C::kStages) & 1) ^ 1);
+          ok = wait(&bars->empty[s], ((n / C::kStages) & 1) ^ 1);
           if (!ok) break;
           if (rank == 0) mbar_arrive_expect_tx(&bars->full[s], PAIR * C::kBytesB);
           unsigned char* b = stages + (size_t)s * C::kStage + kBytesA;
@@ -384,9 +388,10 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
                               at.pl, &bars->full[s]);
         }
       }
-      // copies still in flight must land before the block may exit
+      // copies still in flight must land before the block may exit: used up, or, after a wait that ran out, by the time
+      // that is given to them here
       for (uint32_t m = n > (uint32_t)C::kStages ? n - C::kStages : 0; m < n; ++m)
-        (void)mbar_wait(&bars->empty[m % C::kStages], (m / C::kStages) & 1);
+        (void)mbar_wait(&bars->empty[m % C::kStages], (m / C::kStages) & 1, kLandCycles);
     }
     __syncwarp();
   } else if (warp == 1) {
@@ -400,10 +405,10 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
         for (int j0 = w.k0; j0 < w.k1 && ok; j0 += prm.run, ++nu) {
           const int steps = (min(j0 + prm.run, w.k1) - j0) * prm.planes;
           const uint32_t acc = nu % C::kAccs, d = tmem_base + acc * N;
-          ok = mbar_wait(&bars->acc_empty[acc], ((nu / C::kAccs) & 1) ^ 1);
+          ok = wait(&bars->acc_empty[acc], ((nu / C::kAccs) & 1) ^ 1);
           for (int j = 0; j < steps && ok; ++j, ++n) {
             const int s = n % C::kStages;
-            ok = mbar_wait(&bars->full[s], (n / C::kStages) & 1);
+            ok = wait(&bars->full[s], (n / C::kStages) & 1);
             if (!ok) break;
             tc_fence_after();
             const uint32_t a = smem_u32(stages + (size_t)s * C::kStage), b = a + kBytesA;
@@ -443,8 +448,8 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
       for (int j0 = w.k0; j0 < w.k1;) {
         const bool two_runs = prm.joint && j0 + prm.run < w.k1;
         const uint32_t acc = nu % C::kAccs;
-        ok = __all_sync(0xffffffffu, ok && mbar_wait(&bars->acc_full[acc], (nu / C::kAccs) & 1));
-        if (C::kAccs == 2 && two_runs) ok = __all_sync(0xffffffffu, ok && mbar_wait(&bars->acc_full[acc ^ 1], ((nu + 1) >> 1) & 1));
+        ok = __all_sync(0xffffffffu, ok && wait(&bars->acc_full[acc], (nu / C::kAccs) & 1));
+        if (C::kAccs == 2 && two_runs) ok = __all_sync(0xffffffffu, ok && wait(&bars->acc_full[acc ^ 1], ((nu + 1) >> 1) & 1));
         tc_fence_after();
         for (int c = 0; c < N; c += 32) {
           const uint32_t at_lane = tmem_base + (static_cast<uint32_t>(32 * quarter) << 16) + c;
@@ -483,7 +488,7 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) {
+        if (ok && lane == 0) {
           arrive_first<PAIR>(&bars->acc_empty[acc]);
           if (C::kAccs == 2 && two_runs) arrive_first<PAIR>(&bars->acc_empty[acc ^ 1]);
         }
@@ -504,7 +509,7 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
     }
     for (int n = (warp - 6) >> 2; n < total; n += kConvGroups) {
       const int s = n % C::kStages, r = n % C::kStagesRaw;
-      if (!__all_sync(0xffffffffu, mbar_wait(&bars->raw_full[r], (n / C::kStagesRaw) & 1))) break;
+      if (!__all_sync(0xffffffffu, wait(&bars->raw_full[r], (n / C::kStagesRaw) & 1))) break;
       const unsigned char* raw = raws + (size_t)r * kRawBytes;
       uint2 q[8];
       uint32_t e[8];
@@ -524,7 +529,7 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&bars->raw_empty[r]);     // every lane has its codes
-      if (!__all_sync(0xffffffffu, mbar_wait(&bars->empty[s], ((n / C::kStages) & 1) ^ 1))) break;
+      if (!__all_sync(0xffffffffu, wait(&bars->empty[s], ((n / C::kStages) & 1) ^ 1))) break;
       unsigned char* dst = stages + (size_t)s * C::kStage + to;
 #pragma unroll
       for (int h = 0; h < 8; ++h) *reinterpret_cast<uint4*>(dst + h * 1024) = v[h];
@@ -551,7 +556,7 @@ __global__ void __launch_bounds__(kThreads<SIDE>, 1) weight_grad_kernel(const __
       const uint8_t* column = prm.scales + ((w.i0 >> 5) < prm.scale_pitch ? w.i0 >> 5 : 0);
       for (Steps at(prm, w); at.more(); at.advance(), ++n) {
         const int r = n % C::kStagesRaw;
-        ok = __all_sync(0xffffffffu, mbar_wait(&bars->raw_empty[r], ((n / C::kStagesRaw) & 1) ^ 1));
+        ok = __all_sync(0xffffffffu, wait(&bars->raw_empty[r], ((n / C::kStagesRaw) & 1) ^ 1));
         if (!ok) break;
         if (leader) {
           mbar_arrive_expect_tx(&bars->raw_full[r], kCodeBytes);
@@ -736,6 +741,20 @@ size_t linear_weight_grad_scratch_bytes(long long rows, long long outs, long lon
   return p.pack_bytes + (a > b ? a : b);
 }
 
+namespace {
+std::atomic<long long> g_wait_cycles{kWaitCycles};
+}  // namespace
+
+}  // namespace fa
+
+// Test hook (exported, but deliberately not declared in include/fa.h): shortens the waits of the weight gradient's kernel
+// so that a test can watch them run out on a launch that is otherwise correct.  cycles <= 0 restores the default.
+extern "C" void fa_test_set_weight_grad_wait_cycles(long long cycles) {
+  fa::g_wait_cycles.store(cycles > 0 ? cycles : fa::kWaitCycles);
+}
+
+namespace fa {
+
 template <int N, int PAIR, bool SIDE>
 static cudaError_t launch_product(const CUtensorMap& map, const CUtensorMap& map_codes, const wgrad::Params& prm,
                                   cudaStream_t st) {
@@ -823,6 +842,7 @@ cudaError_t launch_linear_weight_grad(Mat dy, int dtype, long long rows, long lo
   prm.plane = ld * rows;
   prm.columns = dbias ? reinterpret_cast<float*>(room + p.partial_bytes) : nullptr;
   prm.width = p.pitch;
+  prm.wait_cycles = g_wait_cycles.load();
   const bool side = dbias && p.several;
   auto go = [&](auto with_side) {
     constexpr bool SIDE = decltype(with_side)::value;
