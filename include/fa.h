@@ -277,12 +277,13 @@ int fa_gelu_backward(const void* dy, long long lddy, const void* x, long long ld
 /* Gradient of a linear layer's weight and bias from the checkpoint of its input X (rows x ins):
  *   dweight[o][i] = sum over rows t of dy[t][o] * X[t][i]   (outs x ins, contiguous),
  *   dbias[o] = sum over rows t of dy[t][o]                  (NULL: not wanted).
- * rows <= FA_MAX_TOKENS, outs * ins <= 2^40.  Products are exact, sums fp32: the tensor cores' own, which cut off instead
- * of rounding, over at most 1536 (fp32 result) or 4096 (bf16) tokens, and of these rounded to nearest; for inputs of
- * random sign that is 3e-7 and 8e-7 of the result, whatever their number.  A device wait that runs out leaves NaN in
- * the results it concerns.  ws: fa_linear_weight_grad_workspace_bytes(); aligned: non-zero if address and row stride of
- * dy are multiples of 16 bytes and the row stride is at least outs (a bf16 dy is then read where it lies; any other, one
- * row for all included, is laid out in the workspace first). */
+ * rows <= FA_MAX_TOKENS, outs * ins <= 2^40.  Products are exact (of an fp32 dy what lies below 2^-133 is cut off, in dbias
+ * too), sums fp32: the tensor cores' own, which cut off instead of rounding, over at most 1536 (fp32 result) or 4096 (bf16)
+ * tokens, and of these rounded to nearest; for inputs of random sign that is 3e-7 and 8e-7 of the result, whatever their
+ * number.  A device wait that runs out leaves NaN in the results it concerns.  ws:
+ * fa_linear_weight_grad_workspace_bytes(); aligned: non-zero if address and row stride of dy are multiples of 16 bytes and
+ * the row stride is at least outs (a bf16 dy is then read where it lies; any other, one row for all included, is laid out
+ * in the workspace first). */
 #define FA_MAX_TOKENS 2147483520LL     /* 2^31 - 128 */
 int fa_linear_weight_grad_workspace_bytes(long long rows, long long outs, long long ins, int dtype, int aligned,
                                           size_t* bytes);

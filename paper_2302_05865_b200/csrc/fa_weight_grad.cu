@@ -12,7 +12,7 @@
 //   * dY is loaded by TMA straight into that layout;
 //   * a row of the accumulator is one input, so the 32 lanes of a read-out warp hold 32 neighbouring
 //     inputs of one output: stores to dW are coalesced for any alignment of dW.
-// fp32 dY is split into three bf16 terms (8 + 8 + 8 bits, exact) by a pass in front, and the tile is
+// fp32 dY is split into three bf16 terms (8 + 8 + 8 bits, exact down to 2^-133) by a pass in front, and the tile is
 // multiplied with each; the same pass lays out a bf16 dY whose rows TMA cannot address.
 // Few tiles and many tokens: the tokens are split over the blocks, partial products go to scratch in
 // fp32 and a second kernel adds them in a fixed order.
@@ -639,8 +639,9 @@ __global__ void __launch_bounds__(256) finish_kernel(Finish f) {
   }
 }
 
-// dY as bf16 terms that add up to it exactly, rows of `pitch` elements: [planes][rows][pitch].  Terms are
-// cut off rather than rounded, so that no finite value becomes infinite; what is not finite is one term.
+// dY as bf16 terms that add up to it exactly (down to 2^-133, bf16's smallest), rows of `pitch` elements:
+// [planes][rows][pitch].  Terms are cut off rather than rounded, so that no finite value becomes infinite; what is not
+// finite is one term.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) pack_kernel(Source<T> dy, long long rows, int outs,
                                                    int pitch, int planes, bf16* __restrict__ out) {

@@ -38,3 +38,16 @@ def test_one_row_of_dy_for_all_tokens(dtype, rows, outs, ins):
         assert call(f.fa_linear_weight_grad_workspace_bytes(rows, outs, ins, T, aligned=True)) == WORKSPACE
     assert call(f.fa_linear_weight_grad_workspace_bytes(rows, outs, ins, T)) == OK
     assert torch.equal(raw_w, dw) and torch.equal(raw_b, db)
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-34, 1e-36, 1e-38, 1e-41])
+def test_the_smallest_fp32_gradients_are_cut_off_at_a_multiple_of_2_to_the_minus_133(scale):
+    rows, outs, ins = 256, 64, 64
+    g = gen(3)
+    dy = (torch.randn(rows, outs, generator=g, dtype=torch.float64) * scale).float().cuda()
+    ck = fa().fa_checkpoint8_store(randn(g, rows, ins, scale=1e5))
+    x = ref.decode(ck, rows, ins).cuda()
+    dw, db = fa().fa_linear_weight_grad(dy, ck, ins)
+    units = (2 * (rows / 16 + 34) + 16) * 2.0 ** -24              # of the sums, as in the other tests
+    assert ((dw - dy.double().T @ x).abs() <= units * (dy.double().abs().T @ x.abs()) + 2.0 ** -133 * x.abs().sum(0)).all()
+    assert ((db - dy.double().sum(0)).abs() <= (rows / 8 + 128) * 2.0 ** -24 * dy.double().abs().sum(0) + rows * 2.0 ** -133).all()
