@@ -709,9 +709,12 @@ struct LnBackwardGrid {
 LnBackwardGrid ln_backward_grid(bool vec, int dtype, long long rows, long long cols) {
   LnBackwardGrid g{};
   g.s = ln_shape(rows, cols);
-  // bf16: 16384 x 1024 from a checkpoint 42.0 us with one chunk a thread, 41.8 with two; x 1536 58.4 and 54.3; x 2048
-  // 72.6 and 64.5.  An fp32 chunk takes twice the registers on its way: one a thread up to 256 of them.
-  g.is_long = !ln_team(&g.s, vec, dtype == FA_BF16 && vec ? 128 : 256, 1, 2, ln::kMaxKBackward, &g.K);
+  // One chunk a thread up to so many of them, two beyond; from a checkpoint, 16384 rows.  Aligned bf16: of 1024 columns
+  // 39.9 us with one and 37.6 with two, 1536 56.0 and 50.0, 2048 70.3 and 60.4.  Aligned fp32, whose chunk takes twice the
+  // registers: 2048 78.6 and 92.9, 2304 (the least good for one) 120 and 108, 2816 126 and 132, 4096 149 and 196.
+  // Unaligned: fp32 2001 134 and 141, 2305 224 and 173, 4001 282 and 271; bf16 2001 124 and 126, 2305 169 and 155.
+  const int limit = !vec ? 256 : dtype == FA_BF16 ? 128 : 512;
+  g.is_long = !ln_team(&g.s, vec, limit, 1, 2, ln::kMaxKBackward, &g.K);
   long long want;
   if (g.is_long) {
     const long long tiles = (g.s.width + 255) / 256;
