@@ -1,5 +1,10 @@
 // 8-bit activation checkpoints and the element-wise operators around them: store, load, GELU forward
 // (with checkpoints), and GELU backward (from a checkpoint, with the bias gradient).
+// Every value is read and written once.  Store and load are bound by memory, GELU next to it by the instructions a value
+// takes (35 forward with two checkpoints, 26 backward).  Measured on 16384 x 4096, among other calls, bf16 / fp32:
+//   store 37 / 52 us (0.84 / 1.0 of a copy's rate), load 35 / 72 (0.90 / 0.71),
+//   GELU forward with bias and two checkpoints, tanh 89 / 105 (0.70 / 0.98), erf 105 / 214 (0.59 / 0.48: normcdff),
+//   GELU backward from a checkpoint with the bias gradient, tanh 78 / 111 (0.67 / 0.83), erf 90 / 194 (0.57 / 0.48).
 #include "../../include/fa.h"
 #include "fa_columns.cuh"
 #include "fa_train.h"

@@ -8,12 +8,14 @@
 // in registers.  Rows that do not fit (more than 16384 columns forward, 8192 backward) go through the `long` kernels,
 // which read a row several times.
 // Memory is the floor; what holds the kernels above it is the number of instructions a row takes besides its values
-// (sums across lanes and warps, the scales of checkpoints): measured on bf16, 16384 rows of 4096,
-//   forward with residual, sum and two checkpoints 137 us (5.0 TB/s, 0.75 of a copy; 44 instructions a value, 62 % of
-//   the issue slots), backward from a checkpoint with residual gradient 108 + 5 us (4.3 TB/s, 0.64; 33 a value),
-// and of 768: 33 and 35 us (0.59, 0.39).  More chunks a thread spread those instructions over more values, fewer leave
+// (sums across lanes and warps, the scales of checkpoints): measured on bf16, 16384 rows of 4096, among other calls,
+//   forward with residual, sum and two checkpoints 137 us (0.76 of a copy's rate; 44 instructions a value, 63 % of the
+//   issue slots), backward from a checkpoint with residual gradient and column sums 109 us (0.66; 33 a value),
+// and of 768: 31 and 31 us (0.63, 0.43); fp32 rows of 4096 196 and 162 us (0.95, 0.83).  Unaligned rows of 4001, whose
+// shifts are instructions as well: bf16 300 and 290 us, fp32 368 and 340; rows of the `long` kernels (2048 x 20000 bf16,
+// three reads) 144 and 142 us (0.44, 0.31).  More chunks a thread spread those instructions over more values, fewer leave
 // registers for more warps: four (three) chunks are best in the forward pass (768 columns: 33 us, with one 41), one
-// (up to 1024 columns) or two, with two sums a column to keep, in the backward pass.
+// (bf16 up to 1024 columns, fp32 up to 4096) or two, with two sums a column to keep, in the backward pass.
 #include "../../include/fa.h"
 #include "fa_columns.cuh"
 #include "fa_train.h"

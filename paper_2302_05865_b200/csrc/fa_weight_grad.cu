@@ -16,9 +16,10 @@
 // multiplied with each; the same pass lays out a bf16 dY whose rows TMA cannot address.
 // Few tiles and many tokens: the tokens are split over the blocks, partial products go to scratch in
 // fp32 and a second kernel adds them in a fixed order.
-// Shared memory bounds it (see Cfg), and the power limit in a long run.  Measured with the bias gradient, bf16:
-// 4096 x 4096 from 16384 tokens 377 us, 1457 TFLOP/s (439 us in a run of half a second), 4096 x 1024 from 32768 tokens
-// 241 us (278), 768 x 768 from 16384 into fp32 33 us (590 TFLOP/s: 32 steps a pair of blocks, and joining 8 splits).
+// Shared memory bounds it (see Cfg), the read-outs between runs (see kRunF32), and the power limit in a long run.
+// Measured with the bias gradient, bf16: 4096 x 4096 from 16384 tokens 479 us, 1147 TFLOP/s, 4096 x 1024 from 32768
+// tokens 255 us, 1078 TFLOP/s (294 us in a long run), 768 x 768 from 16384 into fp32 33 us (590 TFLOP/s: 32 steps a pair
+// of blocks, and joining 8 splits); an fp32 dY, three products: 4096 x 1024 from 16384 488 us (519 into fp32).
 #include <cuda.h>
 
 #include <atomic>
@@ -259,11 +260,11 @@ struct Steps {
 };
 
 // Column sums of dY while the products run: the tiles that read the same columns share the steps out among themselves,
-// so that every value of dY is read once more, when it is in L2.  (A pass of its own over dY took 46 us next to 234
-// for 4096 x 1024 outputs and inputs of 32768 tokens; this takes 19.)  Four warps: each takes every fourth pair of
+// so that every value of dY is read once more, when it is in L2.  (For 4096 x 1024 outputs and inputs of 32768 tokens
+// this takes 27 us of 263, 20 of 297 with an fp32 result; a pass of its own over dY took 46.)  Four warps: each takes every fourth pair of
 // rows, half a warp (16 chunks of 8 columns) a row, and has sums of its own.
 // They are the read-out warps, which have nothing to do until a unit's products end.  Where a unit is read out in
-// several runs they do have, and four more warps form the sums (SIDE): 275 against 321 us for the shape above in fp32.
+// several runs they do have, and four more warps form the sums (SIDE): 270 against 385 us for the shape above.
 // Elsewhere these would only take registers from the others: 35 against 31 us for 768 x 768 from 16384.
 template <int N, int PAIR>
 struct ColumnSums {
