@@ -17,7 +17,7 @@ pytestmark = pytest.mark.gpu
 
 # tiles of 128 outputs, of 256 by one block and by a pair, of 512; one and several splits, one and several runs; more
 # steps than a ring has stages
-@pytest.mark.parametrize("rows,outs,ins,dtype,gdtype", [(1000, 128, 128, "bf16", "f32"), (600, 200, 136, "f32", "bf16"),
+@pytest.mark.parametrize("rows,outs,ins,dtype,gdtype", [(20000, 128, 128, "bf16", "f32"), (20000, 200, 136, "f32", "bf16"),
                                                        (70000, 300, 120, "bf16", "f32"), (2304, 1024, 1024, "f32", "f32"),
                                                        (6000, 2048, 4096, "bf16", "f32"), (16384, 2048, 4096, "bf16", "bf16")])
 def test_a_wait_that_runs_out_leaves_nan_and_the_next_call_works(rows, outs, ins, dtype, gdtype):
